@@ -200,6 +200,80 @@ size_t kfac_weight_update_workspace_bytes(const kfac_update_item* items_host, in
 int kfac_weight_update_batched(const kfac_update_item* items_host, int32_t count, float eta, float momentum, float eps,
                                void* ws, size_t ws_bytes, void* stream);
 
+/* The step between gradients and their update: the norm over all tensors, and clipping by it.
+ * kfac_grad_norm_batched: *norm (device float) = sqrt(sum of g^2 over all elements of all items), summed in double precision, so that no
+ * finite gradient's square overflows or vanishes; a norm beyond the largest float is given as infinity.
+ * kfac_grad_clip_batched: out = g * min(1, max_norm / norm), each element multiplied in fp32 by the scale rounded to fp32 and rounded to
+ * its type once.  With given_norm = NULL the norm is that of the items, and is written to `norm` as well (ws as for kfac_grad_norm_batched);
+ * else it is read from the device float given_norm (the norm over all processes; what it was computed from is the caller's), `norm` must
+ * be NULL, and ws is not used.  A norm that is not finite leaves the gradients as they are (`norm` tells).  A scale of 1 writes nothing
+ * in place.  Items may differ in every field; those of no elements are skipped; tensors need their elements' alignment only.
+ * max_norm >= 0.  Tensors that are written must not overlap others.  Deterministic: the same items give the same bits. */
+typedef struct kfac_grad_item {
+    const void* g;       /* n gradients, device */
+    void* out;           /* n, device: receives the clipped gradients; NULL or g: in place (g is then written).  Not used by the norm */
+    int64_t n;
+    int32_t dtype;       /* kfac_dtype of g and out */
+} kfac_grad_item;
+
+size_t kfac_grad_norm_workspace_bytes(const kfac_grad_item* items_host, int32_t count);
+int kfac_grad_norm_batched(const kfac_grad_item* items_host, int32_t count, float* norm, void* ws, size_t ws_bytes, void* stream);
+int kfac_grad_clip_batched(const kfac_grad_item* items_host, int32_t count, float max_norm, const float* given_norm, float* norm,
+                           void* ws, size_t ws_bytes, void* stream);
+
+/* Layers of experts.  Each of `tokens` tokens goes to `choices` of `experts` experts; an expert's Kronecker factors are built from its own
+ * tokens, which are brought into the experts' order first.  Where they go is decided on the device, so that nothing here needs a
+ * row count on the host. */
+typedef struct kfac_expert_desc {
+    int32_t tokens;      /* T >= 0; T * choices < 2^31 */
+    int32_t choices;     /* K, 1 .. 64 */
+    int32_t experts;     /* E, 1 .. 1024 */
+    int32_t dim;         /* D: elements of a token's row, 1 .. 2^20 (not used by kfac_expert_sort) */
+    int32_t dtype;       /* kfac_dtype of the rows (not used by kfac_expert_sort) */
+    int64_t ld_token;    /* elements from one row to the next of tensors in tokens' order (x, y, dy); 0: D */
+    int64_t ld_row;      /* the same of tensors in the experts' order (xs, ys, dys), of T K rows; 0: D */
+} kfac_expert_desc;
+
+/* expert: T x K int32.  Assignment i = t K + k goes to row place[i]; expert e's rows are offsets[e] .. offsets[e + 1] - 1, with its
+ * assignments in ascending order; order[row] = i, -1 from row offsets[E] on.  An expert outside 0 .. E - 1 is no assignment: its place is -1.  A token may
+ * name an expert more than once.  offsets: E + 1, order: T K (may be NULL), place: T K int32, device.  ws: 256-byte aligned. */
+size_t kfac_expert_sort_workspace_bytes(const kfac_expert_desc* desc);
+int kfac_expert_sort(const kfac_expert_desc* desc, const int32_t* expert, int32_t* offsets, int32_t* order, int32_t* place, void* ws,
+                     size_t ws_bytes, void* stream);
+
+/* xs[place[t K + k]] = x[t].  Rows that no assignment goes to are left as they are.  A place outside 0 .. T K - 1 is none (here and below).
+ * Its gradient: kfac_expert_combine of the rows' gradients without weights. */
+int kfac_expert_dispatch(const kfac_expert_desc* desc, const void* x, const int32_t* place, void* xs, void* stream);
+
+/* y[t] = sum_k weights[t K + k] ys[place[t K + k]], k ascending, in fp32, rounded once; weights: fp32, NULL: all 1.  A token without
+ * assignments gets zeros; ys and weights of what is no assignment are of no influence. */
+int kfac_expert_combine(const kfac_expert_desc* desc, const void* ys, const float* weights, const int32_t* place, void* y, void* stream);
+
+/* Its gradient: dys[place[t K + k]] = weights[t K + k] dy[t] (other rows are left as they are), dweights[t K + k] = <dy[t], ys[place[t K + k]]>, summed
+ * in fp32, 0 for no assignment.  dweights may be NULL, ys is then not read and may be NULL.  Deterministic. */
+int kfac_expert_combine_backward(const kfac_expert_desc* desc, const void* dy, const void* ys, const float* weights, const int32_t* place,
+                                 void* dys, float* dweights, void* stream);
+
+/* The factors of all experts from rows in the experts' order: F_e = scale * sum_r abar_r abar_r^T over rows offsets[e] .. offsets[e + 1] - 1 of x,
+ * abar_r the row with a trailing 1 if has_bias; scale = 0 selects 1 / (expert e's rows).  d = dim + has_bias.  An expert without rows gets
+ * zeros, and keeps its running average.  A from the experts' inputs, G (has_bias = 0) from their output gradients.  Accumulation as in
+ * kfac_factor_A.  offsets: experts + 1 device int32, ascending, within 0 .. rows (what lies outside is cut off).  x holds `rows` rows; those from offsets[experts] on are not read.
+ * Exactly one of `out` (experts x d x d floats, or experts packed triangles of d (d + 1) / 2) and `running` (experts x d x d: S_e <- decay S_e + (1 - decay) F_e).
+ * Deterministic: the same call gives the same bits. */
+typedef struct kfac_expert_factor_desc {
+    int32_t rows;        /* rows of x, >= 0 */
+    int32_t experts;     /* 1 .. 1024 */
+    int32_t dim;         /* elements of a row, 1 .. 32766 */
+    int32_t dtype;       /* kfac_dtype of x */
+    int32_t has_bias;
+    int32_t packed;      /* 1: `out` receives packed upper triangles (kfac_pack_upper_batched) */
+    int64_t ld;          /* elements from one row to the next; 0: dim.  Rows that do not all begin at 16-byte addresses are copied first */
+} kfac_expert_factor_desc;
+
+size_t kfac_expert_factor_workspace_bytes(const kfac_expert_factor_desc* desc);
+int kfac_expert_factor(const kfac_expert_factor_desc* desc, const void* x, const int32_t* offsets, float scale, float* out, float* running,
+                       float decay, void* ws, size_t ws_bytes, void* stream);
+
 /* Batch Normalization layers (Sec. 5.4: their Fisher matrix is not Kronecker-factorised).  Per-sample gradients of a
  * BN layer's parameters theta = (scale_1..scale_C, shift_1..shift_C):
  *     g[n][c] = sum_s gout[n][s][c] * xhat[n][s][c],   g[n][C + c] = sum_s gout[n][s][c],   s = 0..HW-1,

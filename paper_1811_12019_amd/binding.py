@@ -31,6 +31,9 @@ EXPORTED_SYMBOLS = (
     "kfac_factor_diff_workspace_bytes", "kfac_factor_diff_batched", "kfac_factor_diff_batched_noalloc",
     "kfac_factor_diff_noalloc_max_elements",
     "kfac_weight_update_workspace_bytes", "kfac_weight_update_batched",
+    "kfac_grad_norm_workspace_bytes", "kfac_grad_norm_batched", "kfac_grad_clip_batched",
+    "kfac_expert_sort_workspace_bytes", "kfac_expert_sort", "kfac_expert_dispatch", "kfac_expert_combine",
+    "kfac_expert_combine_backward", "kfac_expert_factor_workspace_bytes", "kfac_expert_factor",
     "kfac_bn_sample_grads_workspace_bytes", "kfac_bn_sample_grads", "kfac_bn_diag_precondition",
     "kfac_bn_sample_grads_batched_workspace_bytes", "kfac_bn_sample_grads_batched",
     "kfac_inverse_workspace_bytes", "kfac_inverse_planes_bytes", "kfac_damped_inverse", "kfac_damped_inverse_batched",
@@ -76,6 +79,20 @@ class kfac_bn_item(ctypes.Structure):
 class kfac_update_item(ctypes.Structure):
     _fields_ = [("w", ctypes.c_void_p), ("w_prev", ctypes.c_void_p), ("precond", ctypes.c_void_p),
                 ("n", ctypes.c_int32), ("d_out", ctypes.c_int32)]
+
+
+class kfac_grad_item(ctypes.Structure):
+    _fields_ = [("g", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
+class kfac_expert_desc(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("tokens", "choices", "experts", "dim", "dtype")] +
+                [("ld_token", ctypes.c_int64), ("ld_row", ctypes.c_int64)])
+
+
+class kfac_expert_factor_desc(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("rows", "experts", "dim", "dtype", "has_bias", "packed")] +
+                [("ld", ctypes.c_int64)])
 
 
 class kfac_inverse_item(ctypes.Structure):
@@ -146,6 +163,27 @@ def load_library() -> ctypes.CDLL:
     lib.kfac_weight_update_workspace_bytes.argtypes = [ctypes.POINTER(kfac_update_item), i32]
     lib.kfac_weight_update_batched.restype = ctypes.c_int
     lib.kfac_weight_update_batched.argtypes = [ctypes.POINTER(kfac_update_item), i32, f32, f32, f32, vp, sz, vp]
+    lib.kfac_grad_norm_workspace_bytes.restype = sz
+    lib.kfac_grad_norm_workspace_bytes.argtypes = [ctypes.POINTER(kfac_grad_item), i32]
+    lib.kfac_grad_norm_batched.restype = ctypes.c_int
+    lib.kfac_grad_norm_batched.argtypes = [ctypes.POINTER(kfac_grad_item), i32, vp, vp, sz, vp]
+    lib.kfac_grad_clip_batched.restype = ctypes.c_int
+    lib.kfac_grad_clip_batched.argtypes = [ctypes.POINTER(kfac_grad_item), i32, f32, vp, vp, vp, sz, vp]
+    expertp, efactorp = ctypes.POINTER(kfac_expert_desc), ctypes.POINTER(kfac_expert_factor_desc)
+    lib.kfac_expert_sort_workspace_bytes.restype = sz
+    lib.kfac_expert_sort_workspace_bytes.argtypes = [expertp]
+    lib.kfac_expert_sort.restype = ctypes.c_int
+    lib.kfac_expert_sort.argtypes = [expertp, vp, vp, vp, vp, vp, sz, vp]
+    lib.kfac_expert_dispatch.restype = ctypes.c_int
+    lib.kfac_expert_dispatch.argtypes = [expertp, vp, vp, vp, vp]
+    lib.kfac_expert_combine.restype = ctypes.c_int
+    lib.kfac_expert_combine.argtypes = [expertp, vp, vp, vp, vp, vp]
+    lib.kfac_expert_combine_backward.restype = ctypes.c_int
+    lib.kfac_expert_combine_backward.argtypes = [expertp, vp, vp, vp, vp, vp, vp, vp]
+    lib.kfac_expert_factor_workspace_bytes.restype = sz
+    lib.kfac_expert_factor_workspace_bytes.argtypes = [efactorp]
+    lib.kfac_expert_factor.restype = ctypes.c_int
+    lib.kfac_expert_factor.argtypes = [efactorp, vp, vp, f32, vp, vp, f32, vp, sz, vp]
     lib.kfac_bn_sample_grads_workspace_bytes.restype = sz
     lib.kfac_bn_sample_grads_workspace_bytes.argtypes = [i32, i32, i32]
     lib.kfac_bn_sample_grads.restype = ctypes.c_int
@@ -408,6 +446,226 @@ def kfac_weight_update_batched(batch: UpdateBatch, eta: float, momentum: float, 
     rc = load_library().kfac_weight_update_batched(batch.host, batch.count, float(eta), float(momentum), float(eps),
                                                    _ptr(batch.ws), ws_bytes, _stream(stream))
     _check(rc, "kfac_weight_update_batched")
+
+
+# The operators below take their sizes from the tensors, so they look at them: another type, shape, stride or device than the call
+# wants raises KfacError with KFAC_ERR_INVALID_ARG before anything is launched.
+_KFAC_DTYPE = {t: k for k, t in _TORCH_DTYPE.items()}
+
+
+def _want(ok: bool, where: str, what: str) -> None:
+    if not ok:
+        raise KfacError(KFAC_ERR_INVALID_ARG, f"{where} ({what})")
+
+
+def _gpu(device, where: str) -> torch.device:
+    """The GPU `device` names, which has to be the current one: the stream a call goes to is the current device's."""
+    device = torch.device(device)
+    _want(device.type == "cuda", where, "tensors of a GPU are wanted")
+    current = torch.cuda.current_device()
+    _want(device.index in (None, current), where, f"the tensors' device {device.index} is not the current one, {current}")
+    return torch.device("cuda", current)
+
+
+def _on_current(device: torch.device, where: str) -> None:
+    current = torch.cuda.current_device()
+    _want(device.index == current, where, f"the tensors' device {device.index} is not the current one, {current}")
+
+
+def _flat(t: torch.Tensor, dtype: torch.dtype, shape, device, where: str, name: str) -> torch.Tensor:
+    _want(t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous() and t.device == device, where,
+          f"{name}: contiguous {dtype} of shape {tuple(shape)} on {device}")
+    return t
+
+
+def _dense(t: torch.Tensor) -> bool:
+    """Whether t's elements lie side by side, in whatever order of dimensions."""
+    step = 1
+    for stride, size in sorted((st, n) for st, n in zip(t.stride(), t.shape) if n != 1):
+        if stride != step:
+            return False
+        step *= size
+    return True
+
+
+class GradBatch:
+    """A kfac_grad_item table (host memory; built once, reused every step), its scratch and the device float `norm`.
+    g: gradient tensors of any of the three types, their elements side by side; out: None (clipped in place), or per tensor None / a
+    tensor of the same type, shape and strides that receives the clipped gradient.  Calls that use one table must not overlap in time."""
+
+    def __init__(self, g: Sequence[torch.Tensor], out: Optional[Sequence[Optional[torch.Tensor]]] = None, device="cuda"):
+        n = len(g)
+        out = [None] * n if out is None else list(out)
+        _want(len(out) == n, "GradBatch", "as many results as gradients")
+        self.device = _gpu(device, "GradBatch")
+        self.count = n
+        self.keep = (list(g), out)
+        self.host = (kfac_grad_item * max(n, 1))()
+        for i, (x, y) in enumerate(zip(g, out)):
+            _want(x.dtype in _KFAC_DTYPE and x.device == self.device and (x.numel() == 0 or _dense(x)), "GradBatch",
+                  f"gradient {i}: float32, bfloat16 or float16 on {self.device}, without gaps")
+            _want(y is None or (y.dtype == x.dtype and y.device == x.device and y.shape == x.shape and y.stride() == x.stride()), "GradBatch",
+                  f"result {i}: the gradient's type, shape and strides")
+            self.host[i] = kfac_grad_item(x.data_ptr(), _ptr(y), x.numel(), _KFAC_DTYPE[x.dtype])
+        self.norm = torch.zeros((), dtype=torch.float32, device=self.device)
+        self.ws = alloc_workspace(int(load_library().kfac_grad_norm_workspace_bytes(self.host, n)), self.device)
+        self.ws_bytes = 0 if self.ws is None else self.ws.numel()
+
+
+def kfac_grad_norm_batched(batch: GradBatch, stream=None) -> torch.Tensor:
+    """The norm over all of the table's gradients: batch.norm, a device float that the next call on the table overwrites."""
+    _on_current(batch.device, "kfac_grad_norm_batched")
+    rc = load_library().kfac_grad_norm_batched(batch.host, batch.count, batch.norm.data_ptr(), _ptr(batch.ws), batch.ws_bytes,
+                                               _stream(stream))
+    _check(rc, "kfac_grad_norm_batched")
+    return batch.norm
+
+
+def kfac_grad_clip_batched(batch: GradBatch, max_norm: float, given_norm: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """out = g min(1, max_norm / norm).  given_norm: None (the norm is that of the table's gradients), or the norm as one device
+    float, such as the norm over all processes.  Returns the norm that was used."""
+    _on_current(batch.device, "kfac_grad_clip_batched")
+    if given_norm is not None:
+        _want(given_norm.dtype == torch.float32 and given_norm.numel() == 1 and given_norm.device == batch.device,
+              "kfac_grad_clip_batched", f"given_norm: one float32 on {batch.device}")
+    norm = batch.norm if given_norm is None else given_norm
+    rc = load_library().kfac_grad_clip_batched(batch.host, batch.count, float(max_norm), _ptr(given_norm),
+                                               None if given_norm is not None else norm.data_ptr(), _ptr(batch.ws), batch.ws_bytes,
+                                               _stream(stream))
+    _check(rc, "kfac_grad_clip_batched")
+    return norm
+
+
+class ExpertRoute:
+    """Where the tokens of a layer of experts go: the device tensors offsets (E + 1), order (T K; None: not wanted) and place (T, K)
+    that kfac_expert_sort fills and the others read, all int32, and the sort's scratch.  Calls that use one object must not
+    overlap a sort in time."""
+
+    def __init__(self, tokens: int, choices: int, experts: int, device="cuda", offsets: Optional[torch.Tensor] = None,
+                 order: Optional[torch.Tensor] = None, place: Optional[torch.Tensor] = None, want_order: bool = True):
+        self.device = _gpu(device, "ExpertRoute")
+        self.tokens, self.choices, self.experts = int(tokens), int(choices), int(experts)
+        self.desc = kfac_expert_desc(self.tokens, self.choices, self.experts, 0, 0, 0, 0)
+        rows = self.tokens * self.choices
+        _want(self.tokens >= 0 and self.choices >= 1 and self.experts >= 1, "ExpertRoute", "tokens, choices, experts")
+        i32 = dict(dtype=torch.int32, device=self.device)
+
+        def given(t, shape, name):
+            return torch.empty(shape, **i32) if t is None else _flat(t, torch.int32, shape, self.device, "ExpertRoute", name)
+
+        self.offsets = given(offsets, (self.experts + 1,), "offsets")
+        self.order = given(order, (rows,), "order") if want_order or order is not None else None
+        self.place = given(place, (self.tokens, self.choices), "place")
+        self.ws = alloc_workspace(int(load_library().kfac_expert_sort_workspace_bytes(ctypes.byref(self.desc))), self.device)
+        self.ws_bytes = 0 if self.ws is None else self.ws.numel()
+        self._descs = {}          # by the tensors' shapes, strides and types
+
+    def _side(self, t, rows, where, name):
+        _want(t.dim() == 2 and t.shape[0] == rows and t.shape[1] >= 1 and t.dtype in _KFAC_DTYPE and t.device == self.device, where,
+              f"{name}: {rows} rows of float32, bfloat16 or float16 on {self.device}")
+        _want(t.shape[1] == 1 or t.stride(1) == 1, where, f"{name}: elements of a row side by side")
+        _want(rows <= 1 or t.stride(0) >= t.shape[1], where, f"{name}: rows apart from each other")
+        return 0 if rows <= 1 else t.stride(0)
+
+    def _rows(self, where, token_side, *row_side):
+        """The descriptor of a call on these tensors (name, tensor)."""
+        key = (where, token_side.shape, token_side.stride(), token_side.dtype, token_side.device,
+               *[(t.shape, t.stride(), t.dtype, t.device) for t in row_side])
+        desc = self._descs.get(key)
+        if desc is None:
+            rows = self.tokens * self.choices
+            ld_token = self._side(token_side, self.tokens, where, "a tensor in tokens' order")
+            ld = [self._side(t, rows, where, "a tensor in the experts' order") for t in row_side]
+            _want(all(t.shape[1] == token_side.shape[1] and t.dtype == token_side.dtype for t in row_side), where, "rows of one width and type")
+            _want(len(set(ld)) == 1, where, "the same stride for both tensors in the experts' order")
+            desc = self._descs[key] = kfac_expert_desc(self.tokens, self.choices, self.experts, token_side.shape[1],
+                                                       _KFAC_DTYPE[token_side.dtype], ld_token, ld[0])
+        _on_current(self.device, where)
+        return ctypes.byref(desc)
+
+    def _weights(self, t, where, name):
+        if t is not None:
+            _want(t.dtype == torch.float32 and t.shape == self.place.shape and t.is_contiguous() and t.device == self.device, where,
+                  f"{name}: contiguous float32 of shape {tuple(self.place.shape)} on {self.device}")
+        return _ptr(t)
+
+
+def kfac_expert_sort(route: ExpertRoute, expert: torch.Tensor, stream=None) -> ExpertRoute:
+    """expert: (T, K) int32, what is not in 0 .. E - 1 is no assignment.  Fills route.offsets, route.order and route.place."""
+    _on_current(route.device, "kfac_expert_sort")
+    _want(expert.dtype == torch.int32 and expert.shape == route.place.shape and expert.is_contiguous() and expert.device == route.device,
+          "kfac_expert_sort", f"expert: contiguous int32 of shape {tuple(route.place.shape)} on {route.device}")
+    rc = load_library().kfac_expert_sort(ctypes.byref(route.desc), expert.data_ptr(), route.offsets.data_ptr(), _ptr(route.order),
+                                         route.place.data_ptr(), _ptr(route.ws), route.ws_bytes, _stream(stream))
+    _check(rc, "kfac_expert_sort")
+    return route
+
+
+def kfac_expert_dispatch(route: ExpertRoute, x: torch.Tensor, xs: torch.Tensor, stream=None) -> torch.Tensor:
+    """x: (T, D), xs: (T K, D): every token's row to its places."""
+    desc = route._rows("kfac_expert_dispatch", x, xs)
+    rc = load_library().kfac_expert_dispatch(desc, x.data_ptr(), route.place.data_ptr(), xs.data_ptr(), _stream(stream))
+    _check(rc, "kfac_expert_dispatch")
+    return xs
+
+
+def kfac_expert_combine(route: ExpertRoute, ys: torch.Tensor, weights: Optional[torch.Tensor], y: torch.Tensor, stream=None) -> torch.Tensor:
+    """ys: (T K, D), weights: (T, K) float32 or None (all 1), y: (T, D).  Without weights also the gradient of kfac_expert_dispatch."""
+    desc = route._rows("kfac_expert_combine", y, ys)
+    rc = load_library().kfac_expert_combine(desc, ys.data_ptr(), route._weights(weights, "kfac_expert_combine", "weights"),
+                                            route.place.data_ptr(), y.data_ptr(), _stream(stream))
+    _check(rc, "kfac_expert_combine")
+    return y
+
+
+def kfac_expert_combine_backward(route: ExpertRoute, dy: torch.Tensor, ys: Optional[torch.Tensor], weights: Optional[torch.Tensor],
+                                 dys: torch.Tensor, dweights: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """dy: (T, D), ys and dys: (T K, D), weights and dweights: (T, K) float32.  dweights = None: ys is not read and may be None."""
+    where = "kfac_expert_combine_backward"
+    _want(dweights is None or ys is not None, where, "dweights needs ys")
+    desc = route._rows(where, dy, dys) if dweights is None else route._rows(where, dy, dys, ys)
+    rc = load_library().kfac_expert_combine_backward(desc, dy.data_ptr(), None if dweights is None else ys.data_ptr(),
+                                                     route._weights(weights, where, "weights"), route.place.data_ptr(), dys.data_ptr(),
+                                                     route._weights(dweights, where, "dweights"), _stream(stream))
+    _check(rc, where)
+    return dys
+
+
+class ExpertFactors:
+    """Descriptor and scratch of the factor builds of one layer of experts (built once, reused every step): x of `rows` rows of `dim`
+    elements of a torch dtype in the experts' order, `ld` elements from one row to the next (0: dim).  Calls that use one object must
+    not overlap in time."""
+
+    def __init__(self, rows: int, experts: int, dim: int, dtype: torch.dtype, has_bias: bool = False, packed: bool = False, ld: int = 0,
+                 device="cuda"):
+        self.device = _gpu(device, "ExpertFactors")
+        _want(dtype in _KFAC_DTYPE, "ExpertFactors", "float32, bfloat16 or float16")
+        self.rows, self.experts, self.dim, self.dtype, self.ld = int(rows), int(experts), int(dim), dtype, int(ld) or int(dim)
+        self.d = self.dim + int(bool(has_bias))
+        self.shape = (self.experts, packed_elems(self.d)) if packed else (self.experts, self.d, self.d)
+        self.desc = kfac_expert_factor_desc(self.rows, self.experts, self.dim, _KFAC_DTYPE[dtype], int(bool(has_bias)), int(bool(packed)), int(ld))
+        self.ws = alloc_workspace(int(load_library().kfac_expert_factor_workspace_bytes(ctypes.byref(self.desc))), self.device)
+        self.ws_bytes = 0 if self.ws is None else self.ws.numel()
+
+
+def kfac_expert_factor(plan: ExpertFactors, x: torch.Tensor, offsets: torch.Tensor, scale: float = 0.0, out: Optional[torch.Tensor] = None,
+                       running: Optional[torch.Tensor] = None, decay: float = 0.0, stream=None) -> torch.Tensor:
+    """The factors of all experts, into `out` (plan.shape, float32), or folded into the running averages `running`."""
+    where = "kfac_expert_factor"
+    _on_current(plan.device, where)
+    _want(x.dtype == plan.dtype and x.shape == (plan.rows, plan.dim) and x.device == plan.device and
+          (plan.dim == 1 or x.stride(1) == 1) and (plan.rows <= 1 or x.stride(0) == plan.ld), where,
+          f"x: {plan.dtype} of shape {(plan.rows, plan.dim)} on {plan.device}, rows {plan.ld} elements apart")
+    _want(offsets.dtype == torch.int32 and offsets.shape == (plan.experts + 1,) and offsets.is_contiguous() and
+          offsets.device == plan.device, where, f"offsets: {plan.experts + 1} contiguous int32 on {plan.device}")
+    _want((out is None) != (running is None), where, "either out or running")
+    to = running if out is None else out
+    _want(to.dtype == torch.float32 and to.shape == plan.shape and to.is_contiguous() and to.device == plan.device, where,
+          f"contiguous float32 results of shape {plan.shape} on {plan.device}")
+    rc = load_library().kfac_expert_factor(ctypes.byref(plan.desc), x.data_ptr(), offsets.data_ptr(), float(scale), _ptr(out), _ptr(running),
+                                           float(decay), _ptr(plan.ws), plan.ws_bytes, _stream(stream))
+    _check(rc, where)
+    return to
 
 
 def kfac_bn_sample_grads_workspace_bytes(N: int, C: int, HW: int) -> int:

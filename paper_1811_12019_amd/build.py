@@ -10,7 +10,7 @@ from concurrent.futures import ThreadPoolExecutor
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libkfac_hip.so")
-SOURCES = ["factor_bf16.hip", "factor_f16.hip", "factor_f32.hip", "factor.hip", "factor_finish.hip", "ema.hip", "packed.hip", "diff.hip", "update.hip", "bn.hip", "inverse.hip", "damping.hip", "precondition.hip", "runtime.hip"]
+SOURCES = ["factor_bf16.hip", "factor_f16.hip", "factor_f32.hip", "factor.hip", "factor_finish.hip", "ema.hip", "packed.hip", "diff.hip", "update.hip", "gradnorm.hip", "experts.hip", "factor_expert.hip", "factor_expert_bf16.hip", "factor_expert_f16.hip", "factor_expert_f32.hip", "bn.hip", "inverse.hip", "damping.hip", "precondition.hip", "runtime.hip"]
 HIPCC_FLAGS = [
     "-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",   # no packed-fp32 VALU ops

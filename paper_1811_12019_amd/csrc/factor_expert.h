@@ -1,0 +1,221 @@
+// The experts' factors: tiles of X_e^T X_e, X_e the rows of expert e, whose bounds lie on the device.  Tile products and epilogues are the matrix-core
+// builder's (factor_tile.h).
+//
+// Cut.  Rows of an expert are cut into ranges of rows_per, which the host chooses from the rows of all experts; how many ranges there are is
+// known on the device only.  A launch has workgroups for the most there can be: rows / rows_per whole ones and a part for every expert, times
+// the tiles.  Every workgroup reads the offsets, adds up the ranges before each expert's (one scan of up to 1024 experts, well below a
+// microsecond against a tile's 10) and finds its own; those behind the last range end.  Ranges of all experts, tiles inside a range, are one work list
+// that is dealt to the XCDs as any build's (unit_of): the tiles of a range, which read the same rows, share an L2.
+// An expert of one range goes straight to its destination; the others' partial sums are added up by a second launch, which there is if
+// an expert can have more than rows_per rows at all.
+// Addresses.  A workgroup takes its range's first row for the tensor's beginning and its last one for the end: offsets inside it fit 32 bits
+// however long x is, and no row of another expert can be read.
+#pragma once
+
+#include "common.h"
+#include "factor_batch.h"
+
+namespace kfac {
+
+struct ExpertArgs {
+    const void* x;           // rows at 16-byte addresses
+    const int* offsets;
+    float* dst;              // the experts' results one after another
+    float* tiles;            // partial sums: [part][ntiles][tile_floats]
+    float* sums;             // column sums: [part][tiles_dim * tw]
+    size_t result;           // floats of an expert's result
+    int rows, experts, dim, dout, ld, dtype, mode;
+    float scale, decay;
+    int rows_per, tw, tiles_dim, ntiles, tile_floats;
+    int ranges, parts;       // the most there can be
+};
+
+constexpr int EXPERT_LDS_INTS = 32;
+
+// What a workgroup works on.
+struct ExpertRange {
+    int expert, sub, ranges; // range `sub` of `ranges` of the expert
+    int part;                // the expert's first partial sum, if it has several ranges
+    int row, rows;           // the expert's rows
+};
+
+// Rows of expert e: offsets that lie outside or descend are cut off.
+__device__ __forceinline__ void expert_rows(const ExpertArgs& a, int e, int& row, int& rows) {
+    const gint* o = as_global((int*)a.offsets);
+    const int r0 = min(max(o[e], 0), a.rows), r1 = min(max(o[e + 1], r0), a.rows);
+    row = r0;
+    rows = r1 - r0;
+}
+
+// Of the ranges of all experts (SPLIT: of the experts of several ranges) the one that `pick` names from their number (-1: none).  False: none.
+template <bool SPLIT, class Pick>
+__device__ __forceinline__ bool expert_range(const ExpertArgs& a, int* lds, Pick&& pick, ExpertRange& out) {
+    const int t = threadIdx.x, nt = blockDim.x, lane = t & 63, wave = t >> 6, waves = nt >> 6;
+    const int per = (a.experts + nt - 1) / nt, e0 = t * per;
+    unsigned key = 0, part = 0;                                        // of this thread's experts
+    auto ranges_of = [&](int e, int& row, int& rows) -> int {
+        expert_rows(a, e, row, rows);
+        const int n = (int)(((unsigned)rows + a.rows_per - 1) / (unsigned)a.rows_per);
+        return n == 0 && a.mode != OUT_EMA ? 1 : n;                    // (an average without rows stays as it is)
+    };
+    for (int e = e0; e < e0 + per && e < a.experts; ++e) {
+        int row, rows;
+        const unsigned n = ranges_of(e, row, rows);
+        key += SPLIT ? (n > 1) : n;
+        part += n > 1 ? n : 0;
+    }
+    unsigned k = key, p = part;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const unsigned ku = __shfl_up(k, off, 64), pu = __shfl_up(p, off, 64);
+        if (lane >= off) {
+            k += ku;
+            p += pu;
+        }
+    }
+    if (lane == 63) {
+        lds[wave] = (int)k;
+        lds[8 + wave] = (int)p;
+    }
+    __syncthreads();
+    unsigned all = 0, kb = 0, pb = 0;
+    for (int w = 0; w < waves; ++w) {
+        if (w < wave) {
+            kb += (unsigned)lds[w];
+            pb += (unsigned)lds[8 + w];
+        }
+        all += (unsigned)lds[w];
+    }
+    if (all > (unsigned)a.ranges) all = (unsigned)a.ranges;            // (offsets that do not ascend could name more)
+    const int want = pick((int)all);                                   // (the same in all threads)
+    if (want < 0 || (unsigned)want >= all) return false;
+    kb += k - key;
+    pb += p - part;
+    if ((unsigned)want >= kb && (unsigned)want < kb + key) {
+        for (int e = e0;; ++e) {                                       // (ends inside this thread's experts)
+            int row, rows;
+            const unsigned n = ranges_of(e, row, rows), mine = SPLIT ? (n > 1) : n;
+            if ((unsigned)want < kb + mine) {
+                lds[16] = e;
+                lds[17] = want - (int)kb;
+                lds[18] = (int)n;
+                lds[19] = (int)pb;
+                lds[20] = row;
+                lds[21] = rows;
+                break;
+            }
+            kb += mine;
+            pb += n > 1 ? n : 0;
+        }
+    }
+    __syncthreads();
+    out.expert = __builtin_amdgcn_readfirstlane(lds[16]);
+    out.sub = __builtin_amdgcn_readfirstlane(lds[17]);
+    out.ranges = __builtin_amdgcn_readfirstlane(lds[18]);
+    out.part = __builtin_amdgcn_readfirstlane(lds[19]);
+    out.row = __builtin_amdgcn_readfirstlane(lds[20]);
+    out.rows = __builtin_amdgcn_readfirstlane(lds[21]);
+    return out.ranges == 1 || (long long)out.part + out.ranges <= a.parts;
+}
+
+// `rows` rows, all of them an expert's or a range of its R rows, as the matrix-core builder sees them.
+__host__ __device__ __forceinline__ View expert_view(const ExpertArgs& a, int rows, int R) {
+    View v;
+    Unfold& u = v.u;
+    u.N = rows;
+    u.C = v.run = a.ld;
+    u.H = u.W = u.Ho = u.Wo = u.kh = u.kw = u.stride = 1;
+    u.pad = 0;
+    u.has_bias = a.dout > a.dim;
+    u.layout = KFAC_NHWC;
+    u.dtype = a.dtype;
+    u.order = KFAC_ORDER_KH_KW_C;
+    u.R = R;
+    u.d = v.cout = a.dim;
+    v.dout = a.dout;
+    v.kw = 1;
+    v.chunked = v.mapped = v.repack = v.rows = v.shared = v.planes = 0;
+    return v;
+}
+__device__ __forceinline__ float expert_scale(const ExpertArgs& a, int rows) {
+    return a.scale != 0.f ? a.scale : rows > 0 ? 1.f / (float)rows : 0.f;
+}
+__device__ __forceinline__ OutSpec expert_out(const ExpertArgs& a, int expert) {
+    OutSpec o;
+    o.dst = as_global(a.dst) + (size_t)expert * a.result;
+    o.decay = a.decay;
+    o.one_minus = 1.f - a.decay;
+    o.mode = a.mode;
+    return o;
+}
+
+// (the tile kernel's launch bounds: factor_launch.h)
+template <int TW, int KIND>
+__global__ __launch_bounds__((tile_threads<TW, KIND == 2 ? 4 : 2>())) __attribute__((amdgpu_waves_per_eu(TW == 256 || KIND == 2 ? 2 : 3, 8)))
+void expert_tile_kernel(ExpertArgs a) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    constexpr int ES = KIND == 2 ? 4 : 2;
+    ExpertRange r;
+    int tile = 0;
+    const bool there = expert_range<false>(a, (int*)(smem + tile_lds_bytes<TW, ES>()), [&](int all) {
+        const int unit = unit_of(all * a.ntiles, blockIdx.x, 0);
+        const int range = unit < 0 ? -1 : unit / a.ntiles;
+        tile = unit - range * a.ntiles;
+        return range;
+    }, r);
+    if (!there) return;                                                // (uniform)
+    const int first = r.sub * a.rows_per, count = min(a.rows_per, r.rows - first);
+    const View v = expert_view(a, count, r.rows);
+    TileJob job;
+    tri_decode_blocked<4>(a.tiles_dim, tile, job.I, job.J);
+    job.r_begin = 0;
+    job.r_end = count;
+    job.scale = expert_scale(a, r.rows);
+    job.split = r.ranges > 1;
+    job.lower = a.ntiles == 1;
+    const size_t part = (size_t)r.part + r.sub;
+    job.tile_dst = as_global(a.tiles) + (part * a.ntiles + tile) * a.tile_floats;
+    job.sums_dst = as_global(a.sums) + part * (a.tiles_dim * a.tw);
+    job.first_pixel = job.partner = 0;
+    const KFAC_AS1 unsigned char* x = (const KFAC_AS1 unsigned char*)a.x + (size_t)(r.row + first) * a.ld * ES;
+    const OutSpec os = expert_out(a, r.expert);
+    if (job.I == job.J) {
+        if (TW == 128 && a.tw == 64) factor_tile_run<TW == 128 ? 64 : TW, KIND, FEED_PIXELS, true>(v, x, job, os, smem);
+        else factor_tile_run<TW, KIND, FEED_PIXELS, true>(v, x, job, os, smem);
+    } else {
+        factor_tile_run<TW, KIND, FEED_PIXELS, false>(v, x, job, os, smem);
+    }
+}
+
+template <int TW, int KIND>
+static int launch_expert_tile_kernel(const char* name, const ExpertArgs& a, unsigned wgs, hipStream_t stream) {
+    constexpr int ES = KIND == 2 ? 4 : 2, LDS = tile_lds_bytes<TW, ES>() + EXPERT_LDS_INTS * 4;
+    if constexpr (LDS > 64 * 1024) {                                   // (see launch_tile_kernel)
+        if (hipFuncSetAttribute((const void*)expert_tile_kernel<TW, KIND>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess)
+            return KFAC_ERR_HIP;
+    }
+    void* tok = nullptr;
+    if (timing_enabled()) timing_begin(name, stream, &tok);
+    hipLaunchKernelGGL((expert_tile_kernel<TW, KIND>), dim3(wgs), dim3(tile_threads<TW, ES>()), LDS, stream, a);
+    if (tok) timing_end(stream, tok);
+    if (hipGetLastError() != hipSuccess) return KFAC_ERR_HIP;
+    return KFAC_OK;
+}
+
+// KIND 0: bf16, 1: fp16, 2: fp32 (one to a source file).
+template <int KIND>
+int launch_expert_tiles(const ExpertArgs& a, unsigned wgs, hipStream_t stream)
+#ifdef KFAC_EXPERT_KIND
+{
+    if constexpr (KIND != 2) {
+        if (a.tw == 256) return launch_expert_tile_kernel<256, KIND>("expert_tile_kernel<256, 16-bit>", a, wgs, stream);
+        return launch_expert_tile_kernel<128, KIND>("expert_tile_kernel<128, 16-bit>", a, wgs, stream);
+    }
+    return launch_expert_tile_kernel<128, KIND>("expert_tile_kernel<128, f32>", a, wgs, stream);
+}
+template int launch_expert_tiles<KFAC_EXPERT_KIND>(const ExpertArgs&, unsigned, hipStream_t);
+#else
+    ;
+#endif
+
+}  // namespace kfac

@@ -1,0 +1,283 @@
+// The norm over the gradients of many tensors, and clipping by it:
+//     norm = sqrt(sum g^2),   out = g min(1, max_norm / norm).
+// HBM bound: a gradient's bytes once for the norm, twice more for the clipping.  Launches:
+//   grad_partial_kernel   up to NORM_WGS workgroups in all, each a run of consecutive 4096-element chunks; a double each
+//   grad_norm_kernel      (the norm alone) adds those up
+//   grad_clip_kernel      every workgroup adds them up itself, in the same order, which saves the launch between
+// Squares are added in double precision: fp32 squares of bf16 or fp32 gradients beyond 1.8e19 overflow, and those below 1e-23 vanish.
+#include "rows16.h"
+
+namespace kfac {
+
+constexpr int GN_MAX = 128;               // tensors per launch (an argument block of 3.7 KB)
+constexpr unsigned GN_CHUNK = 4096;       // elements
+constexpr int NORM_WGS = 1024;            // four workgroups to a CU
+constexpr int CLIP_WGS = 2048;
+
+struct GradBatch {
+    int count;
+    unsigned prefix[GN_MAX + 1];          // first chunk of tensor i
+    unsigned char dtype[GN_MAX];
+    unsigned long long n[GN_MAX];
+    const void* g[GN_MAX];
+    void* out[GN_MAX];
+};
+
+// The workgroup's run of chunks, tensor by tensor: f(tensor, first element, behind the last one).
+template <class F>
+__device__ __forceinline__ void for_run(const GradBatch& b, F&& f) {
+    const int t = threadIdx.x;
+    const unsigned chunks = b.prefix[b.count];
+    const unsigned c0 = (unsigned)((unsigned long long)chunks * blockIdx.x / gridDim.x);
+    const unsigned c1 = (unsigned)((unsigned long long)chunks * (blockIdx.x + 1) / gridDim.x);
+    int m = __syncthreads_count(t < b.count - 1 && b.prefix[t + 1] <= c0);
+    for (; m < b.count && b.prefix[m] < c1; ++m) {
+        const unsigned first = b.prefix[m];
+        const unsigned long long from = c0 > first ? (unsigned long long)(c0 - first) * GN_CHUNK : 0;
+        const unsigned long long n = b.n[m], to = (unsigned long long)(c1 - first) * GN_CHUNK;
+        f(m, from, to < n ? to : n);
+    }
+}
+
+template <int KIND>
+__device__ __forceinline__ double square_run(const gchar* g, unsigned long long count) {
+    constexpr int V = elems16<KIND>, ES = elem_bytes<KIND>;
+    const int t = threadIdx.x;
+    double s = 0.0;
+    auto add = [&](const u4& r) {
+        float x[V];
+        unpack16<KIND>(r, x);
+#pragma unroll
+        for (int i = 0; i < V; ++i) s = fma((double)x[i], (double)x[i], s);
+    };
+    const unsigned long long vecs = count / V;
+    unsigned long long v = t;
+    for (; v + 3 * 256 < vecs; v += 4 * 256) {
+        u4 r[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r[j] = load_row16<ES>(g + (v + j * 256) * 16, V);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) add(r[j]);
+    }
+    for (; v < vecs; v += 256) add(load_row16<ES>(g + v * 16, V));
+    if (t == 0 && count % V) add(load_row16<ES>(g + vecs * 16, (int)(count % V)));
+    return s;
+}
+
+__global__ __launch_bounds__(256) void grad_partial_kernel(GradBatch b, double* partial) {
+    __shared__ double red[4];
+    const int t = threadIdx.x;
+    double s = 0.0;
+    for_run(b, [&](int m, unsigned long long from, unsigned long long to) {
+        const gchar* g = (const gchar*)b.g[m];
+        const int dt = b.dtype[m];
+        if (dt == KFAC_F32) s += square_run<2>(g + from * 4, to - from);
+        else if (dt == KFAC_BF16) s += square_run<0>(g + from * 2, to - from);
+        else s += square_run<1>(g + from * 2, to - from);
+    });
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) s += __shfl_down(s, off, 64);
+    if ((t & 63) == 0) red[t >> 6] = s;
+    __syncthreads();
+    if (t == 0) partial[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+// All 256 threads get the sum of n doubles, added in an order that depends on n alone.
+__device__ __forceinline__ double sum_of(const double* partial, int n, double* red) {
+    const int t = threadIdx.x;
+    double s = 0.0;
+    for (int c = t; c < n; c += 256) s += partial[c];
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) s += __shfl_down(s, off, 64);
+    if ((t & 63) == 0) red[t >> 6] = s;
+    __syncthreads();
+    return (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+__global__ __launch_bounds__(256) void grad_norm_kernel(const double* partial, int n, float* norm) {
+    __shared__ double red[4];
+    const double s = sum_of(partial, n, red);
+    if (threadIdx.x == 0) *norm = (float)sqrt(s);
+}
+
+template <int KIND>
+__device__ __forceinline__ void clip_run(const gchar* g, gchar* out, unsigned long long count, float scale) {
+    constexpr int V = elems16<KIND>, ES = elem_bytes<KIND>;
+    const int t = threadIdx.x;
+    auto scaled = [&](const u4& r) {
+        float x[V];
+        unpack16<KIND>(r, x);
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] *= scale;
+        return pack16<KIND>(x);
+    };
+    const unsigned long long vecs = count / V;
+    unsigned long long v = t;
+    for (; v + 3 * 256 < vecs; v += 4 * 256) {
+        u4 r[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r[j] = load_row16<ES>(g + (v + j * 256) * 16, V);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) store_row16<ES>(out + (v + j * 256) * 16, scaled(r[j]), V);
+    }
+    for (; v < vecs; v += 256) store_row16<ES>(out + v * 16, scaled(load_row16<ES>(g + v * 16, V)), V);
+    if (t == 0 && count % V) store_row16<ES>(out + vecs * 16, scaled(load_row16<ES>(g + vecs * 16, (int)(count % V))), (int)(count % V));
+}
+
+__global__ __launch_bounds__(256) void grad_clip_kernel(GradBatch b, const double* partial, int n, const float* given, float max_norm, float* norm) {
+    __shared__ double red[4];
+    double len;
+    if (given) {
+        len = (double)*given;
+    } else {
+        len = sqrt(sum_of(partial, n, red));
+        if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)len;
+    }
+    const float scale = len > (double)max_norm && len < __builtin_inf() ? (float)((double)max_norm / len) : 1.f;
+    for_run(b, [&](int m, unsigned long long from, unsigned long long to) {
+        const gchar* g = (const gchar*)b.g[m];
+        gchar* out = (gchar*)b.out[m];
+        if (scale == 1.f && g == out) return;
+        const int dt = b.dtype[m];
+        if (dt == KFAC_F32) clip_run<2>(g + from * 4, out + from * 4, to - from, scale);
+        else if (dt == KFAC_BF16) clip_run<0>(g + from * 2, out + from * 2, to - from, scale);
+        else clip_run<1>(g + from * 2, out + from * 2, to - from, scale);
+    });
+}
+
+static size_t gn_elem_bytes(int dtype) { return dtype == KFAC_F32 ? 4 : 2; }
+static unsigned long long gn_chunks(int64_t n) { return ((unsigned long long)n + GN_CHUNK - 1) / GN_CHUNK; }
+
+constexpr unsigned long long GN_MOST_CHUNKS = 1ull << 31;   // 2^43 elements
+
+// Chunks of all items; 0 if one of them is not valid or they are too many.
+static bool gn_total(const kfac_grad_item* items, int count, unsigned long long* total) {
+    *total = 0;
+    for (int i = 0; i < count; ++i) {
+        const kfac_grad_item& it = items[i];
+        if (it.n < 0 || it.n >= (int64_t)(GN_MOST_CHUNKS * GN_CHUNK)) return false;
+        *total += gn_chunks(it.n);
+        if (*total >= GN_MOST_CHUNKS) return false;
+    }
+    return true;
+}
+
+// Launches: the next up to GN_MAX items that have elements, as a batch; returns its chunks (0: no more items).
+static unsigned gn_fill(const kfac_grad_item* items, int count, int* next, GradBatch* b) {
+    b->count = 0;
+    b->prefix[0] = 0;
+    for (; *next < count && b->count < GN_MAX; ++*next) {
+        const kfac_grad_item& it = items[*next];
+        if (it.n == 0) continue;
+        const int k = b->count++;
+        b->prefix[k + 1] = b->prefix[k] + (unsigned)gn_chunks(it.n);
+        b->dtype[k] = (unsigned char)it.dtype;
+        b->n[k] = (unsigned long long)it.n;
+        b->g[k] = it.g;
+        b->out[k] = it.out ? it.out : const_cast<void*>(it.g);
+    }
+    return b->prefix[b->count];
+}
+
+// Workgroups of a launch over `chunks` of `total` chunks, `wgs` for all of them.
+static unsigned gn_wgs(unsigned chunks, unsigned long long total, int wgs) {
+    unsigned long long n = total <= (unsigned long long)wgs ? chunks : ((unsigned long long)chunks * wgs + total - 1) / total;
+    return (unsigned)(n < chunks ? n : chunks);
+}
+
+// Workgroups, and doubles, of the first pass.
+static int gn_partials(const kfac_grad_item* items, int count, unsigned long long total) {
+    int n = 0;
+    unsigned chunks = 0;
+    int in_launch = 0;
+    for (int i = 0; i <= count; ++i) {
+        if (i == count || in_launch == GN_MAX) {
+            if (chunks) n += (int)gn_wgs(chunks, total, NORM_WGS);
+            chunks = 0;
+            in_launch = 0;
+            if (i == count) break;
+        }
+        if (items[i].n == 0) continue;
+        chunks += (unsigned)gn_chunks(items[i].n);
+        ++in_launch;
+    }
+    return n;
+}
+
+static int gn_check(const kfac_grad_item* items, int32_t count, bool clip) {
+    if (count < 0 || (count > 0 && !items)) return KFAC_ERR_INVALID_ARG;
+    for (int i = 0; i < count; ++i) {
+        const kfac_grad_item& it = items[i];
+        if (it.dtype != KFAC_F32 && it.dtype != KFAC_BF16 && it.dtype != KFAC_F16) return KFAC_ERR_INVALID_ARG;
+        if (it.n < 0) return KFAC_ERR_INVALID_ARG;
+        if (it.n == 0) continue;
+        const size_t es = gn_elem_bytes(it.dtype);
+        if (!it.g || (uintptr_t)it.g % es) return KFAC_ERR_INVALID_ARG;
+        if (clip && it.out && it.out != it.g) {
+            const uintptr_t a = (uintptr_t)it.g, b = (uintptr_t)it.out, bytes = (uintptr_t)it.n * es;
+            if (b % es || (a < b + bytes && b < a + bytes)) return KFAC_ERR_INVALID_ARG;
+        }
+    }
+    unsigned long long total;
+    return gn_total(items, count, &total) ? KFAC_OK : KFAC_ERR_TOO_LARGE;
+}
+
+static int gn_first_pass(const kfac_grad_item* items, int count, unsigned long long total, double* partial, int* n, hipStream_t stream) {
+    GradBatch b;
+    *n = 0;
+    for (int next = 0; unsigned chunks = gn_fill(items, count, &next, &b);) {
+        const unsigned wgs = gn_wgs(chunks, total, NORM_WGS);
+        KFAC_LAUNCH(grad_partial_kernel, dim3(wgs), dim3(256), stream, b, partial + *n);
+        *n += (int)wgs;
+    }
+    return KFAC_OK;
+}
+
+}  // namespace kfac
+
+using namespace kfac;
+
+extern "C" size_t kfac_grad_norm_workspace_bytes(const kfac_grad_item* items_host, int32_t count) {
+    unsigned long long total;
+    if (!items_host || count <= 0 || !gn_total(items_host, count, &total)) return 0;
+    return align_up((size_t)gn_partials(items_host, count, total) * sizeof(double), 256);
+}
+
+extern "C" int kfac_grad_norm_batched(const kfac_grad_item* items_host, int32_t count, float* norm, void* ws, size_t ws_bytes, void* stream) {
+    int rc = gn_check(items_host, count, false);
+    if (rc != KFAC_OK) return rc;
+    if (!norm || (uintptr_t)norm % 4) return KFAC_ERR_INVALID_ARG;
+    unsigned long long total;
+    gn_total(items_host, count, &total);
+    if (total && (!ws || ((uintptr_t)ws & 255) || ws_bytes < kfac_grad_norm_workspace_bytes(items_host, count))) return KFAC_ERR_WORKSPACE;
+    int n;
+    rc = gn_first_pass(items_host, count, total, (double*)ws, &n, (hipStream_t)stream);
+    if (rc != KFAC_OK) return rc;
+    KFAC_LAUNCH(grad_norm_kernel, dim3(1), dim3(256), (hipStream_t)stream, (const double*)ws, n, norm);
+    return KFAC_OK;
+}
+
+extern "C" int kfac_grad_clip_batched(const kfac_grad_item* items_host, int32_t count, float max_norm, const float* given_norm, float* norm,
+                                      void* ws, size_t ws_bytes, void* stream) {
+    int rc = gn_check(items_host, count, true);
+    if (rc != KFAC_OK) return rc;
+    if (!(max_norm >= 0.f) || (given_norm ? norm != nullptr : norm == nullptr)) return KFAC_ERR_INVALID_ARG;
+    if ((uintptr_t)given_norm % 4 || (uintptr_t)norm % 4) return KFAC_ERR_INVALID_ARG;
+    unsigned long long total;
+    gn_total(items_host, count, &total);
+    if (!given_norm && total && (!ws || ((uintptr_t)ws & 255) || ws_bytes < kfac_grad_norm_workspace_bytes(items_host, count))) return KFAC_ERR_WORKSPACE;
+    hipStream_t st = (hipStream_t)stream;
+    int n = 0;
+    if (!given_norm) {
+        rc = gn_first_pass(items_host, count, total, (double*)ws, &n, st);
+        if (rc != KFAC_OK) return rc;
+        if (!total) {                                          // no elements: a norm of 0
+            KFAC_LAUNCH(grad_norm_kernel, dim3(1), dim3(256), st, (const double*)ws, 0, norm);
+            return KFAC_OK;
+        }
+    }
+    GradBatch b;
+    for (int next = 0; unsigned chunks = gn_fill(items_host, count, &next, &b);)
+        KFAC_LAUNCH(grad_clip_kernel, dim3(gn_wgs(chunks, total, CLIP_WGS)), dim3(256), st, b, (const double*)ws, n, given_norm, max_norm, norm);
+    return KFAC_OK;
+}

@@ -1,0 +1,152 @@
+"""The norm over many gradients, and clipping by it, against the float64 oracle.
+
+Tolerances, u = 2^-24: the norm is summed in double precision (relative error far below u) and rounded to fp32 once: 1.001 u.  A clipped value is
+multiplied in fp32 by the scale rounded to fp32 and rounded to its type: 2.001 u, and half a step of a 16-bit type (2^-8, 2^-11) on top,
+or half its smallest number."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import experts_oracle as eo
+from paper_1811_12019_amd import binding as kb
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+U = 2.0 ** -24
+HALF = {torch.float32: 0.0, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+TINY = {torch.float32: 2.0 ** -149, torch.bfloat16: 2.0 ** -133, torch.float16: 2.0 ** -24}
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def grads(sizes, types, seed, scale=1e-2, off=0):
+    """Tensors of the given numbers of elements, `off` elements into their own storage."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    return [(torch.randn((n + off,), generator=g, device=DEV) * scale).to(types[i % len(types)])[off:] for i, n in enumerate(sizes)]
+
+
+def check(got, norm, tensors, max_norm, given=None):
+    want, want_norm = eo.grad_clip([f64(t) for t in tensors], max_norm, given)
+    if given is None:
+        assert abs(float(norm) - want_norm) <= 1.001 * U * want_norm
+    for i, (a, b, t) in enumerate(zip(got, want, tensors)):
+        assert (np.abs(f64(a) - b) <= (2.001 * U + HALF[t.dtype]) * np.abs(b) * (1 + HALF[t.dtype]) + TINY[t.dtype]).all(), i
+
+
+CASES = [([1], [F32], 0), ([1], [BF16], 0), ([7], [F16], 1), ([0, 5, 0], [F32], 0), ([4096], [F32], 0), ([4097], [BF16], 0), ([8191, 3, 1, 100], [F16, F32], 0),
+         ([100000, 1, 4095, 4096, 70000], [BF16, F32, F16], 3), ([3 + i % 50 for i in range(128)], [F32], 0), ([1 + i % 7 for i in range(129)], [BF16], 1),
+         ([(37 * i) % 9001 for i in range(700)], [F32, BF16, F16], 1), ([5000000, 17], [BF16], 0), ([3000001, 2000000, 11], [F32], 2), ([0] * 5, [F32], 0)]
+
+
+@pytest.mark.parametrize("into", ["place", "others", "mixed"])
+@pytest.mark.parametrize("sizes,types,off", CASES, ids=lambda v: str(v)[:24])
+def test_norm_and_clip(sizes, types, off, into):
+    tensors = grads(sizes, types, len(sizes), off=off)
+    before = [t.clone() for t in tensors]
+    size = eo.grad_norm([f64(t) for t in before])
+    for max_norm in (0.37 * size, 2 * size + 1, 0.0):
+        for t, b in zip(tensors, before):
+            t.copy_(b)
+        out = None if into == "place" else [None if into == "mixed" and i % 2 else torch.full_like(t, 77.0) for i, t in enumerate(tensors)]
+        batch = kb.GradBatch(tensors, out)
+        norm = kb.kfac_grad_norm_batched(batch).clone()
+        assert abs(float(norm) - size) <= 1.001 * U * size
+        used = kb.kfac_grad_clip_batched(batch, max_norm)
+        assert torch.equal(used, norm)
+        got = [t if out is None or out[i] is None else out[i] for i, t in enumerate(tensors)]
+        check(got, norm, before, max_norm)
+        if max_norm > size:
+            assert all(torch.equal(a, b) for a, b in zip(got, before))
+        for i, (t, b) in enumerate(zip(tensors, before)):
+            if out is not None and out[i] is not None:
+                assert torch.equal(t, b)
+
+
+def test_a_given_norm():
+    tensors = grads([1000, 33], [F32, BF16], 1)
+    before = [t.clone() for t in tensors]
+    batch = kb.GradBatch(tensors)
+    given = torch.tensor([3.0], device=DEV)
+    assert kb.kfac_grad_clip_batched(batch, 2.0, given) is given
+    check(tensors, None, before, 2.0, 3.0)
+    for bad in (float("nan"), float("inf"), 1.0):
+        kept = [t.clone() for t in tensors]
+        kb.kfac_grad_clip_batched(batch, 2.0, torch.tensor(bad, device=DEV))
+        assert all(torch.equal(a, b) for a, b in zip(tensors, kept)), bad
+
+
+@pytest.mark.parametrize("scale", [1e30, 1e-30])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_squares_beyond_fp32(dtype, scale):
+    tensors = grads([5000, 70], [dtype], 2, scale=scale)
+    before = [t.clone() for t in tensors]
+    norm = kb.kfac_grad_clip_batched(kb.GradBatch(tensors), 0.25 * scale)
+    check(tensors, norm, before, 0.25 * scale)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_a_norm_that_is_not_finite_clips_nothing(dtype, bad):
+    tensors = grads([5000, 70, 3], [dtype], 3)
+    tensors[1][69] = bad
+    before = [t.clone() for t in tensors]
+    out = [torch.zeros_like(t) for t in tensors]
+    norm = kb.kfac_grad_clip_batched(kb.GradBatch(tensors, out), 1e-3)
+    assert bool(norm.isnan()) == (bad != bad) and not bool(norm.isfinite())
+    for a, b in zip(out, before):
+        assert torch.equal(torch.nan_to_num(a), torch.nan_to_num(b)) and torch.equal(a.isnan(), b.isnan())
+
+
+def test_gradients_in_other_orders_of_dimensions():
+    g = torch.randn((4, 3, 5, 6), device=DEV).to(memory_format=torch.channels_last)
+    out = torch.zeros_like(g)
+    kb.kfac_grad_clip_batched(kb.GradBatch([g], [out]), 1.0)
+    check([out], kb.kfac_grad_norm_batched(kb.GradBatch([g])), [g], 1.0)
+    for bad in (lambda: kb.GradBatch([g[:, :2]]), lambda: kb.GradBatch([g], [out.contiguous()]), lambda: kb.GradBatch([g], [out.bfloat16()]),
+                lambda: kb.GradBatch([g.double()]), lambda: kb.GradBatch([g.cpu()]), lambda: kb.GradBatch([g], []), lambda: kb.GradBatch([g[:1].expand(4, 3, 5, 6)]),
+                lambda: kb.kfac_grad_clip_batched(kb.GradBatch([g]), -1.0), lambda: kb.kfac_grad_clip_batched(kb.GradBatch([g]), 1.0, torch.zeros(2, device=DEV)),
+                lambda: kb.kfac_grad_clip_batched(kb.GradBatch([g]), 1.0, torch.zeros(1))):
+        with pytest.raises(kb.KfacError):
+            bad()
+
+
+def test_more_than_four_gigabytes_in_one_tensor():
+    n = (1 << 31) + 4101
+    g = torch.ones(n, dtype=BF16, device=DEV)
+    g[-3:] = 2.0
+    batch = kb.GradBatch([g])
+    size = np.sqrt(float(n - 3) + 12.0)
+    norm = kb.kfac_grad_clip_batched(batch, float(size / 4))
+    assert abs(float(norm) - size) <= 1.001 * U * size
+    assert bool((g[:-3] == 0.25).all()) and g[-3:].tolist() == [0.5] * 3     # (1 / 4 and a scale within 2 u of it round alike)
+
+
+def test_captured_and_replayed():
+    sizes = [30000, 1, 500, 77777]
+    a, b = grads(sizes, [F32, BF16], 0), grads(sizes, [F32, BF16], 0)
+    out_a, out_b = [torch.zeros_like(t) for t in a], [torch.zeros_like(t) for t in b]
+    one, two = kb.GradBatch(a, out_a), kb.GradBatch(b, out_b)
+    kb.kfac_grad_clip_batched(one, 0.5)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kb.kfac_grad_clip_batched(one, 0.5)
+    for seed in range(1, 5):
+        for t, v in zip(a + b, 2 * grads(sizes, [F32, BF16], seed, scale=10.0 ** -seed)):
+            t.copy_(v)
+        graph.replay()
+        kb.kfac_grad_clip_batched(two, 0.5)
+        torch.cuda.synchronize()
+        assert torch.equal(one.norm, two.norm) and all(torch.equal(x, y) for x, y in zip(out_a, out_b))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_deterministic(dtype):
+    tensors = grads([100003, 50000, 999], [dtype], 5)
+    batch = kb.GradBatch(tensors)
+    first = kb.kfac_grad_norm_batched(batch).clone()
+    for _ in range(3):
+        assert torch.equal(kb.kfac_grad_norm_batched(batch), first)
