@@ -467,9 +467,13 @@ def _gpu(device, where: str) -> torch.device:
     return torch.device("cuda", current)
 
 
-def _on_current(device: torch.device, where: str) -> None:
-    current = torch.cuda.current_device()
-    _want(device.index == current, where, f"the tensors' device {device.index} is not the current one, {current}")
+def _stream_on(index: int, where: str, stream) -> int:
+    """The stream of a call on tensors of GPU `index`, which has to be the current one."""
+    get = getattr(torch._C, "_cuda_getDevice", None)
+    current = torch.cuda.current_device() if get is None else get()
+    if current != index:
+        _want(False, where, f"the tensors' device {index} is not the current one, {current}")
+    return _stream(stream)
 
 
 def _flat(t: torch.Tensor, dtype: torch.dtype, shape, device, where: str, name: str) -> torch.Tensor:
@@ -514,9 +518,8 @@ class GradBatch:
 
 def kfac_grad_norm_batched(batch: GradBatch, stream=None) -> torch.Tensor:
     """The norm over all of the table's gradients: batch.norm, a device float that the next call on the table overwrites."""
-    _on_current(batch.device, "kfac_grad_norm_batched")
     rc = load_library().kfac_grad_norm_batched(batch.host, batch.count, batch.norm.data_ptr(), _ptr(batch.ws), batch.ws_bytes,
-                                               _stream(stream))
+                                               _stream_on(batch.device.index, "kfac_grad_norm_batched", stream))
     _check(rc, "kfac_grad_norm_batched")
     return batch.norm
 
@@ -524,15 +527,14 @@ def kfac_grad_norm_batched(batch: GradBatch, stream=None) -> torch.Tensor:
 def kfac_grad_clip_batched(batch: GradBatch, max_norm: float, given_norm: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """out = g min(1, max_norm / norm).  given_norm: None (the norm is that of the table's gradients), or the norm as one device
     float, such as the norm over all processes.  Returns the norm that was used."""
-    _on_current(batch.device, "kfac_grad_clip_batched")
-    if given_norm is not None:
-        _want(given_norm.dtype == torch.float32 and given_norm.numel() == 1 and given_norm.device == batch.device,
-              "kfac_grad_clip_batched", f"given_norm: one float32 on {batch.device}")
+    where = "kfac_grad_clip_batched"
+    if given_norm is not None and not (given_norm.dtype == torch.float32 and given_norm.numel() == 1 and given_norm.device == batch.device):
+        _want(False, where, f"given_norm: one float32 on {batch.device}")
     norm = batch.norm if given_norm is None else given_norm
     rc = load_library().kfac_grad_clip_batched(batch.host, batch.count, float(max_norm), _ptr(given_norm),
                                                None if given_norm is not None else norm.data_ptr(), _ptr(batch.ws), batch.ws_bytes,
-                                               _stream(stream))
-    _check(rc, "kfac_grad_clip_batched")
+                                               _stream_on(batch.device.index, where, stream))
+    _check(rc, where)
     return norm
 
 
@@ -544,6 +546,7 @@ class ExpertRoute:
     def __init__(self, tokens: int, choices: int, experts: int, device="cuda", offsets: Optional[torch.Tensor] = None,
                  order: Optional[torch.Tensor] = None, place: Optional[torch.Tensor] = None, want_order: bool = True):
         self.device = _gpu(device, "ExpertRoute")
+        self.index = self.device.index
         self.tokens, self.choices, self.experts = int(tokens), int(choices), int(experts)
         self.desc = kfac_expert_desc(self.tokens, self.choices, self.experts, 0, 0, 0, 0)
         rows = self.tokens * self.choices
@@ -568,9 +571,10 @@ class ExpertRoute:
         return 0 if rows <= 1 else t.stride(0)
 
     def _rows(self, where, token_side, *row_side):
-        """The descriptor of a call on these tensors (name, tensor)."""
-        key = (where, token_side.shape, token_side.stride(), token_side.dtype, token_side.device,
-               *[(t.shape, t.stride(), t.dtype, t.device) for t in row_side])
+        """The descriptor of a call on these tensors."""
+        key = (token_side.shape, token_side.stride(), token_side.dtype, token_side.get_device())
+        for t in row_side:
+            key += (t.shape, t.stride(), t.dtype, t.get_device())
         desc = self._descs.get(key)
         if desc is None:
             rows = self.tokens * self.choices
@@ -578,25 +582,25 @@ class ExpertRoute:
             ld = [self._side(t, rows, where, "a tensor in the experts' order") for t in row_side]
             _want(all(t.shape[1] == token_side.shape[1] and t.dtype == token_side.dtype for t in row_side), where, "rows of one width and type")
             _want(len(set(ld)) == 1, where, "the same stride for both tensors in the experts' order")
-            desc = self._descs[key] = kfac_expert_desc(self.tokens, self.choices, self.experts, token_side.shape[1],
-                                                       _KFAC_DTYPE[token_side.dtype], ld_token, ld[0])
-        _on_current(self.device, where)
-        return ctypes.byref(desc)
+            desc = self._descs[key] = ctypes.byref(kfac_expert_desc(self.tokens, self.choices, self.experts, token_side.shape[1],
+                                                                    _KFAC_DTYPE[token_side.dtype], ld_token, ld[0]))
+        return desc
 
     def _weights(self, t, where, name):
-        if t is not None:
-            _want(t.dtype == torch.float32 and t.shape == self.place.shape and t.is_contiguous() and t.device == self.device, where,
-                  f"{name}: contiguous float32 of shape {tuple(self.place.shape)} on {self.device}")
-        return _ptr(t)
+        if t is None:
+            return None
+        if not (t.dtype == torch.float32 and t.shape == self.place.shape and t.is_contiguous() and t.get_device() == self.index):
+            _want(False, where, f"{name}: contiguous float32 of shape {tuple(self.place.shape)} on {self.device}")
+        return t.data_ptr()
 
 
 def kfac_expert_sort(route: ExpertRoute, expert: torch.Tensor, stream=None) -> ExpertRoute:
     """expert: (T, K) int32, what is not in 0 .. E - 1 is no assignment.  Fills route.offsets, route.order and route.place."""
-    _on_current(route.device, "kfac_expert_sort")
-    _want(expert.dtype == torch.int32 and expert.shape == route.place.shape and expert.is_contiguous() and expert.device == route.device,
-          "kfac_expert_sort", f"expert: contiguous int32 of shape {tuple(route.place.shape)} on {route.device}")
+    if not (expert.dtype == torch.int32 and expert.shape == route.place.shape and expert.is_contiguous() and expert.get_device() == route.index):
+        _want(False, "kfac_expert_sort", f"expert: contiguous int32 of shape {tuple(route.place.shape)} on {route.device}")
     rc = load_library().kfac_expert_sort(ctypes.byref(route.desc), expert.data_ptr(), route.offsets.data_ptr(), _ptr(route.order),
-                                         route.place.data_ptr(), _ptr(route.ws), route.ws_bytes, _stream(stream))
+                                         route.place.data_ptr(), _ptr(route.ws), route.ws_bytes,
+                                         _stream_on(route.index, "kfac_expert_sort", stream))
     _check(rc, "kfac_expert_sort")
     return route
 
@@ -604,7 +608,8 @@ def kfac_expert_sort(route: ExpertRoute, expert: torch.Tensor, stream=None) -> E
 def kfac_expert_dispatch(route: ExpertRoute, x: torch.Tensor, xs: torch.Tensor, stream=None) -> torch.Tensor:
     """x: (T, D), xs: (T K, D): every token's row to its places."""
     desc = route._rows("kfac_expert_dispatch", x, xs)
-    rc = load_library().kfac_expert_dispatch(desc, x.data_ptr(), route.place.data_ptr(), xs.data_ptr(), _stream(stream))
+    rc = load_library().kfac_expert_dispatch(desc, x.data_ptr(), route.place.data_ptr(), xs.data_ptr(),
+                                             _stream_on(route.index, "kfac_expert_dispatch", stream))
     _check(rc, "kfac_expert_dispatch")
     return xs
 
@@ -613,7 +618,7 @@ def kfac_expert_combine(route: ExpertRoute, ys: torch.Tensor, weights: Optional[
     """ys: (T K, D), weights: (T, K) float32 or None (all 1), y: (T, D).  Without weights also the gradient of kfac_expert_dispatch."""
     desc = route._rows("kfac_expert_combine", y, ys)
     rc = load_library().kfac_expert_combine(desc, ys.data_ptr(), route._weights(weights, "kfac_expert_combine", "weights"),
-                                            route.place.data_ptr(), y.data_ptr(), _stream(stream))
+                                            route.place.data_ptr(), y.data_ptr(), _stream_on(route.index, "kfac_expert_combine", stream))
     _check(rc, "kfac_expert_combine")
     return y
 
@@ -626,7 +631,7 @@ def kfac_expert_combine_backward(route: ExpertRoute, dy: torch.Tensor, ys: Optio
     desc = route._rows(where, dy, dys) if dweights is None else route._rows(where, dy, dys, ys)
     rc = load_library().kfac_expert_combine_backward(desc, dy.data_ptr(), None if dweights is None else ys.data_ptr(),
                                                      route._weights(weights, where, "weights"), route.place.data_ptr(), dys.data_ptr(),
-                                                     route._weights(dweights, where, "dweights"), _stream(stream))
+                                                     route._weights(dweights, where, "dweights"), _stream_on(route.index, where, stream))
     _check(rc, where)
     return dys
 
@@ -639,6 +644,7 @@ class ExpertFactors:
     def __init__(self, rows: int, experts: int, dim: int, dtype: torch.dtype, has_bias: bool = False, packed: bool = False, ld: int = 0,
                  device="cuda"):
         self.device = _gpu(device, "ExpertFactors")
+        self.index = self.device.index
         _want(dtype in _KFAC_DTYPE, "ExpertFactors", "float32, bfloat16 or float16")
         self.rows, self.experts, self.dim, self.dtype, self.ld = int(rows), int(experts), int(dim), dtype, int(ld) or int(dim)
         self.d = self.dim + int(bool(has_bias))
@@ -652,18 +658,17 @@ def kfac_expert_factor(plan: ExpertFactors, x: torch.Tensor, offsets: torch.Tens
                        running: Optional[torch.Tensor] = None, decay: float = 0.0, stream=None) -> torch.Tensor:
     """The factors of all experts, into `out` (plan.shape, float32), or folded into the running averages `running`."""
     where = "kfac_expert_factor"
-    _on_current(plan.device, where)
-    _want(x.dtype == plan.dtype and x.shape == (plan.rows, plan.dim) and x.device == plan.device and
-          (plan.dim == 1 or x.stride(1) == 1) and (plan.rows <= 1 or x.stride(0) == plan.ld), where,
-          f"x: {plan.dtype} of shape {(plan.rows, plan.dim)} on {plan.device}, rows {plan.ld} elements apart")
-    _want(offsets.dtype == torch.int32 and offsets.shape == (plan.experts + 1,) and offsets.is_contiguous() and
-          offsets.device == plan.device, where, f"offsets: {plan.experts + 1} contiguous int32 on {plan.device}")
+    if not (x.dtype == plan.dtype and x.shape == (plan.rows, plan.dim) and x.get_device() == plan.index and
+            (plan.dim == 1 or x.stride(1) == 1) and (plan.rows <= 1 or x.stride(0) == plan.ld)):
+        _want(False, where, f"x: {plan.dtype} of shape {(plan.rows, plan.dim)} on {plan.device}, rows {plan.ld} elements apart")
+    if not (offsets.dtype == torch.int32 and offsets.shape == (plan.experts + 1,) and offsets.is_contiguous() and offsets.get_device() == plan.index):
+        _want(False, where, f"offsets: {plan.experts + 1} contiguous int32 on {plan.device}")
     _want((out is None) != (running is None), where, "either out or running")
     to = running if out is None else out
-    _want(to.dtype == torch.float32 and to.shape == plan.shape and to.is_contiguous() and to.device == plan.device, where,
-          f"contiguous float32 results of shape {plan.shape} on {plan.device}")
+    if not (to.dtype == torch.float32 and to.shape == plan.shape and to.is_contiguous() and to.get_device() == plan.index):
+        _want(False, where, f"contiguous float32 results of shape {plan.shape} on {plan.device}")
     rc = load_library().kfac_expert_factor(ctypes.byref(plan.desc), x.data_ptr(), offsets.data_ptr(), float(scale), _ptr(out), _ptr(running),
-                                           float(decay), _ptr(plan.ws), plan.ws_bytes, _stream(stream))
+                                           float(decay), _ptr(plan.ws), plan.ws_bytes, _stream_on(plan.index, where, stream))
     _check(rc, where)
     return to
 

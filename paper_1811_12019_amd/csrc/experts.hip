@@ -7,145 +7,120 @@
 // 64 assignments of a step among themselves: the lanes of the same expert are found bit by bit with ballots, and their number below a
 // lane is its rank.  No atomics that return a value: the order is the assignments'.  Runs of one workgroup need one launch.
 // Rows.  HBM bound.  A thread takes 16 bytes of a token's row, so that x, y and dy are touched once, whatever the number of choices.
+#include <algorithm>
+
 #include "rows16.h"
 
 namespace kfac {
+
+template <bool B> struct BoolConstant { static constexpr bool value = B; };
+template <int N> struct IntConstant { static constexpr int value = N; };
 
 constexpr int EX_MAX_EXPERTS = 1024, EX_MAX_CHOICES = 64, EX_MAX_DIM = 1 << 20;
 
 struct SortCut {
     int blocks, waves, per_wave;          // assignments of a wavefront, a multiple of 64
     int bits;                             // of an expert's number
+    int width;                            // threads of the second kernel that read a run's counts, 8 each: a power of two
     int lds;                              // bytes of the second kernel
 };
-constexpr int SORT_STEPS = 4, SORT_BLOCKS = 256, SORT_ALONE = 8192;
+constexpr int SORT_STEPS = 2, SORT_STEPS_MANY = 8, SORT_BLOCKS = 256, SORT_ALONE = 6144;
+constexpr long long SORT_RUN_MAX = 32768;  // counts have 16 bits
 
 static SortCut sort_cut(int n, int experts) {
     SortCut c;
-    c.waves = experts <= 512 ? 16 : 8;    // (counts of every wavefront in LDS)
-    const long long run = (long long)c.waves * 64 * SORT_STEPS;
-    long long blocks = n <= SORT_ALONE ? 1 : (n + run - 1) / run;
-    if (blocks > SORT_BLOCKS) blocks = SORT_BLOCKS;
+    const int most = experts <= 512 ? 16 : 8;                 // (counts of every wavefront in LDS)
+    long long blocks = 1;
+    c.waves = most;
+    if (n <= SORT_ALONE) {                                    // one workgroup, of as few wavefronts as have something to do
+        const int want = std::max((n + 64 * SORT_STEPS - 1) / (64 * SORT_STEPS), (experts + 255) / 256);
+        c.waves = std::min(std::max(want, 1), most);
+    } else {
+        const long long run = (long long)most * 64;
+        blocks = std::max(std::min((n + run - 1) / run, (long long)SORT_BLOCKS), (n + SORT_RUN_MAX - 1) / SORT_RUN_MAX);
+    }
     const long long per = (n + blocks * c.waves - 1) / (blocks * c.waves);
-    c.per_wave = (int)((per + 63) / 64 * 64);
-    if (c.per_wave < 64) c.per_wave = 64;
-    c.blocks = (int)((n + (long long)c.per_wave * c.waves - 1) / ((long long)c.per_wave * c.waves));
-    if (c.blocks < 1) c.blocks = 1;
+    c.per_wave = std::max((int)((per + 63) / 64 * 64), 64);
+    const long long run = (long long)c.per_wave * c.waves;
+    c.blocks = (int)std::max((n + run - 1) / run, 1ll);
     c.bits = 0;
     while ((1 << c.bits) < experts) ++c.bits;
-    c.lds = (c.waves * experts + 2 * experts + 2 * c.waves * 64 + 32) * 4;
+    c.width = 1;
+    while (c.width * 8 < experts) c.width *= 2;
+    c.lds = (c.waves * experts + 2 * c.width * 8 + 1) * 4;
     return c;
 }
 
-// A run's experts, counted: counts[blockIdx][e].
-__global__ __launch_bounds__(1024) void expert_count_kernel(const int* expert, int n, int experts, int per_block, int* counts) {
+// A run's experts, counted: counts[blockIdx][e], 8 * width of them.
+__global__ __launch_bounds__(1024) void expert_count_kernel(const int* expert, int n, int experts, int per_block, int width, uint16_t* counts) {
     __shared__ int cnt[EX_MAX_EXPERTS];
     const int t = threadIdx.x, nt = blockDim.x;
-    for (int e = t; e < experts; e += nt) cnt[e] = 0;
+    for (int e = t; e < 8 * width; e += nt) cnt[e] = 0;
     __syncthreads();
     const long long i0 = (long long)blockIdx.x * per_block, i1 = i0 + per_block < n ? i0 + per_block : n;
+#pragma unroll 4
     for (long long i = i0 + t; i < i1; i += nt) {
         const int e = expert[i];
         if ((unsigned)e < (unsigned)experts) atomicAdd(&cnt[e], 1);
     }
     __syncthreads();
-    for (int e = t; e < experts; e += nt) counts[(size_t)blockIdx.x * experts + e] = cnt[e];
+    for (int e = t; e < 8 * width; e += nt) counts[(size_t)blockIdx.x * (8 * width) + e] = (uint16_t)cnt[e];
 }
 
-__global__ __launch_bounds__(1024) void expert_place_kernel(const int* expert, int n, int experts, int per_wave, int bits, const int* counts,
-                                                            int* offsets, int* order, int* place) {
+// STEPS: a wavefront's assignments and their ranks stay in registers (0: are looked up again).
+template <int STEPS>
+__global__ __launch_bounds__(1024) void expert_place_kernel(const int* expert, int n, int experts, int per_wave, int bits, int width,
+                                                            const uint16_t* counts, int* offsets, int* order, int* place) {
     extern __shared__ int lds[];
     const int t = threadIdx.x, nt = blockDim.x, lane = t & 63, wave = t >> 6, waves = nt >> 6;
-    int* cnt = lds;                                     // [waves][experts]: a wavefront's counts, then where its next rows go
-    int* total = cnt + waves * experts;                 // [experts]: of all runs, then the expert's first row
-    int* before = total + experts;                      // [experts]: of the runs before this one
-    int* red = before + experts;                        // [2][nt]
-    int* scan = red + 2 * nt;                           // [waves] and the number of rows
+    int* cnt = lds;                                     // [waves][experts]: a wavefront's counts, then where its rows go
+    int* total = cnt + waves * experts;                 // [8 width], at(e): of all runs, then the expert's first row
+    int* before = total + 8 * width;                    // the same of the runs before this one
+    int* all_rows = before + 8 * width;
+    auto at = [&](int e) { return (e & 7) * width + (e >> 3); };   // (neighbouring threads' eights in neighbouring banks)
     const int blk = blockIdx.x, nblk = gridDim.x;
-    for (int e = t; e < waves * experts; e += nt) cnt[e] = 0;
-    __syncthreads();
     const long long i0 = ((long long)blk * waves + wave) * per_wave, i1 = i0 + per_wave < n ? i0 + per_wave : n;
-    for (long long i = i0 + lane; i < i1; i += 64) {
-        const int e = expert[i];
-        if ((unsigned)e < (unsigned)experts) atomicAdd(&cnt[wave * experts + e], 1);
-    }
-    if (nblk > 1) {                                     // thread groups share out the runs
-        const int width = (experts + 63) & ~63, groups = width <= nt ? nt / width : 1;
-        for (int e0 = 0; e0 < experts; e0 += groups > 1 ? experts : nt) {
-            const int g = groups > 1 ? t / width : 0, e = e0 + (groups > 1 ? t % width : t);
-            int all = 0, mine = 0;
-            if (g < groups && e < experts) {
-#pragma unroll 8
-                for (int b = g; b < nblk; b += groups) {
-                    const int c = counts[(size_t)b * experts + e];
-                    all += c;
-                    mine += b < blk ? c : 0;
-                }
-            }
-            red[t] = all;
-            red[nt + t] = mine;
-            __syncthreads();
-            if (g == 0 && e < experts) {
-                for (int k = 1; k < groups; ++k) {
-                    all += red[k * width + t];
-                    mine += red[nt + k * width + t];
-                }
-                total[e] = all;
-                before[e] = mine;
-            }
-            __syncthreads();
-        }
-    } else {
-        __syncthreads();
-        for (int e = t; e < experts; e += nt) {
-            int all = 0;
-            for (int w = 0; w < waves; ++w) all += cnt[w * experts + e];
-            total[e] = all;
-            before[e] = 0;
-        }
-        __syncthreads();
-    }
-    // the experts' first rows: an exclusive scan, two experts to a thread
-    {
-        const int a = 2 * t < experts ? total[2 * t] : 0, b = 2 * t + 1 < experts ? total[2 * t + 1] : 0;
-        int s = a + b;
+    constexpr int HELD = STEPS ? STEPS : 1;
+    int held[HELD], rank[HELD];
+    if constexpr (STEPS > 0) {
 #pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const int up = __shfl_up(s, off, 64);
-            if (lane >= off) s += up;
-        }
-        if (lane == 63) scan[wave] = s;
-        __syncthreads();
-        int base = 0, rows = 0;
-        for (int w = 0; w < waves; ++w) {
-            if (w < wave) base += scan[w];
-            rows += scan[w];
-        }
-        const int first = base + s - a - b;
-        if (2 * t < experts) total[2 * t] = first;
-        if (2 * t + 1 < experts) total[2 * t + 1] = first + a;
-        if (t == 0) scan[waves] = rows;
+        for (int k = 0; k < STEPS; ++k) held[k] = i0 + 64 * k + lane < i1 ? expert[i0 + 64 * k + lane] : -1;
     }
-    __syncthreads();
-    const int rows = scan[waves];
-    if (blk == 0) {
-        for (int e = t; e < experts; e += nt) offsets[e] = total[e];
-        if (t == 0) offsets[experts] = rows;
-    }
-    for (int e = t; e < experts; e += nt) {
-        int at = total[e] + before[e];
-        for (int w = 0; w < waves; ++w) {
-            const int c = cnt[w * experts + e];
-            cnt[w * experts + e] = at;
-            at += c;
+    for (int e = t; e < waves * experts + 16 * width; e += nt) cnt[e] = 0;
+    // The counts of all runs and of those before this one: groups of `width` threads share out the runs, a thread takes 8 experts.
+    int all[8] = {}, some[8] = {};
+    const int col = t & (width - 1), groups = nt / width;
+    if (nblk > 1) {
+#pragma unroll 4
+        for (int b = t / width; b < nblk; b += groups) {
+            const u4 c = *(const KFAC_AS1 u4*)((const gchar*)counts + ((size_t)b * width + col) * 16);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int v = (int)(c[k / 2] >> (k & 1) * 16 & 0xffff);
+                all[k] += v;
+                some[k] += b < blk ? v : 0;
+            }
+        }
+        for (int off = width; off < 64; off <<= 1) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                all[k] += __shfl_xor(all[k], off, 64);
+                some[k] += __shfl_xor(some[k], off, 64);
+            }
         }
     }
     __syncthreads();
-    int* next = cnt + wave * experts;
+    if (nblk > 1 && lane < width) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (all[k]) atomicAdd(&total[k * width + col], all[k]);
+            if (some[k]) atomicAdd(&before[k * width + col], some[k]);
+        }
+    }
+    // Lanes of the same expert among the 64, and where the wavefront's earlier ones end: the lane's rank.  Counts them.
+    int* mine = cnt + wave * experts;
     const unsigned long long below = (1ull << lane) - 1;
-    for (long long i = i0; i < i1; i += 64) {
-        const bool in = i + lane < i1;
-        const int e = in ? expert[i + lane] : -1;
+    auto rank_of = [&](int e) -> int {
         const bool there = (unsigned)e < (unsigned)experts;
         unsigned long long same = __ballot(there);
         for (int k = 0; k < bits; ++k) {
@@ -153,13 +128,91 @@ __global__ __launch_bounds__(1024) void expert_place_kernel(const int* expert, i
             const unsigned long long set = __ballot(bit);
             same &= bit ? set : ~set;
         }
-        int row = -1;
-        if (there) row = next[e] + __popcll(same & below);
+        int r = -1;
+        if (there) r = mine[e] + __popcll(same & below);
         __builtin_amdgcn_wave_barrier();                // (all have read before one of an expert's lanes writes)
-        if (there && (same & below) == 0) next[e] += __popcll(same);
+        if (there && (same & below) == 0) mine[e] += __popcll(same);
         __builtin_amdgcn_wave_barrier();
-        if (in) place[i + lane] = row;
-        if (there && order) order[row] = (int)(i + lane);
+        return r;
+    };
+    if constexpr (STEPS > 0) {
+#pragma unroll
+        for (int k = 0; k < STEPS; ++k) rank[k] = i0 + 64 * k < i1 ? rank_of(held[k]) : -1;
+    } else {
+#pragma unroll 8
+        for (long long i = i0 + lane; i < i1; i += 64) {
+            const int e = expert[i];
+            if ((unsigned)e < (unsigned)experts) atomicAdd(&mine[e], 1);
+        }
+    }
+    __syncthreads();
+    // The experts' first rows: an exclusive scan by one wavefront, some experts to a lane.  Beside it (of one run: before it) the others go
+    // from counts to what lies before a wavefront's rows.
+    auto scan = [&]() {
+        const int per = (experts + 63) >> 6, e0 = lane * per;
+        int own = 0;
+        for (int k = 0; k < per; ++k) own += e0 + k < experts ? total[at(e0 + k)] : 0;
+        int s = own;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int up = __shfl_up(s, off, 64);
+            if (lane >= off) s += up;
+        }
+        int first = s - own;
+        for (int k = 0; k < per && e0 + k < experts; ++k) {
+            const int c = total[at(e0 + k)];
+            total[at(e0 + k)] = first;
+            first += c;
+        }
+        if (lane == 63) *all_rows = s;
+    };
+    const int helpers = nblk > 1 ? 64 : 0;              // (threads that scan meanwhile; several runs have at least 8 wavefronts)
+    if (t < helpers) {
+        scan();
+    } else {
+        for (int e = t - helpers; e < experts; e += nt - helpers) {
+            int sum = 0;
+#pragma unroll 8
+            for (int w = 0; w < waves; ++w) {
+                const int c = cnt[w * experts + e];
+                cnt[w * experts + e] = sum;
+                sum += c;
+            }
+            if (nblk == 1) total[at(e)] = sum;
+        }
+    }
+    __syncthreads();
+    if (nblk == 1) {
+        if (wave == 0) scan();
+        __syncthreads();
+    }
+    const int rows = *all_rows;
+    if (blk == 0) {
+        for (int e = t; e < experts; e += nt) offsets[e] = total[at(e)];
+        if (t == 0) offsets[experts] = rows;
+    }
+    if constexpr (STEPS > 0) {
+#pragma unroll
+        for (int k = 0; k < STEPS; ++k) {
+            const long long i = i0 + 64 * k + lane;
+            const int e = max(held[k], 0);
+            const bool there = rank[k] >= 0;
+            const int row = there ? total[at(e)] + before[at(e)] + mine[e] + rank[k] : -1;
+            if (i < i1) place[i] = row;
+            if (there && order) order[row] = (int)i;
+        }
+    } else {
+        for (int e = lane; e < experts; e += 64) mine[e] += total[at(e)] + before[at(e)];
+        __builtin_amdgcn_wave_barrier();
+        int next = i0 + lane < i1 ? expert[i0 + lane] : -1;
+        for (long long i = i0; i < i1; i += 64) {
+            const bool in = i + lane < i1;
+            const int e = next;
+            next = i + 64 + lane < i1 ? expert[i + 64 + lane] : -1;
+            const int row = rank_of(e);
+            if (in) place[i + lane] = row;
+            if (row >= 0 && order) order[row] = (int)(i + lane);
+        }
     }
     if (order)
         for (long long p = rows + (long long)blk * nt + t; p < n; p += (long long)nblk * nt) order[p] = -1;
@@ -172,74 +225,138 @@ struct RowArgs {
     long long ld_token, ld_row;           // bytes
 };
 
-template <int ES>
+// The last vector of a row may hold fewer elements than the others: f(true) where it does not, so that the loads of f can all be on their way at
+// a time (a load under a condition of its own is waited for before the next one).
+template <int V, class F>
+__device__ __forceinline__ void by_whole(int left, F&& f) {
+    if (left >= V) f(BoolConstant<true>{});
+    else f(BoolConstant<false>{});
+}
+
+constexpr int GROUP = 4;                  // choices whose rows are fetched together
+constexpr unsigned BACK_WORKGROUP = 256;  // vectors of a row from which on a whole workgroup takes a token
+constexpr int BACK_FEW = 512;
+
+template <int ES, bool STREAM>
 __global__ __launch_bounds__(256) void expert_dispatch_kernel(RowArgs a, const char* x, const int* place, char* xs) {
     const unsigned i = blockIdx.x * 256u + threadIdx.x;
     if (i >= a.vectors) return;
     const unsigned token = i / a.per_row, c = i - token * a.per_row;
     const int left = a.dim - (int)c * (16 / ES);
-    const u4 r = load_row16<ES>((const gchar*)x + token * a.ld_token + c * 16ll, left);
     const gint* p = as_global((int*)place) + (size_t)token * a.choices;
-    for (int k = 0; k < a.choices; ++k) {
-        const int row = p[k];
-        if ((unsigned)row < (unsigned)a.rows) store_row16<ES>((gchar*)xs + row * a.ld_row + c * 16ll, r, left);
-    }
+    by_whole<16 / ES>(left, [&](auto whole) {
+        const int count = decltype(whole)::value ? 16 / ES : left;
+        const u4 r = load_row16<ES>((const gchar*)x + token * a.ld_token + c * 16ll, count);
+        for (int k = 0; k < a.choices; ++k) {
+            const int row = p[k];
+            if ((unsigned)row < (unsigned)a.rows) store_row16<ES, STREAM>((gchar*)xs + row * a.ld_row + c * 16ll, r, count);
+        }
+    });
 }
 
-template <int KIND>
+template <int KIND, bool STREAM>
 __global__ __launch_bounds__(256) void expert_combine_kernel(RowArgs a, const char* ys, const float* weights, const int* place, char* y) {
     constexpr int ES = elem_bytes<KIND>, V = elems16<KIND>;
     const unsigned i = blockIdx.x * 256u + threadIdx.x;
     if (i >= a.vectors) return;
     const unsigned token = i / a.per_row, c = i - token * a.per_row;
     const int left = a.dim - (int)c * V;
-    const size_t at = (size_t)token * a.choices;
-    float sum[V] = {};
-    for (int k = 0; k < a.choices; ++k) {
-        const int row = place[at + k];
-        if ((unsigned)row >= (unsigned)a.rows) continue;
-        const float w = weights ? weights[at + k] : 1.f;
-        float f[V];
-        unpack16<KIND>(load_row16<ES>((const gchar*)ys + row * a.ld_row + c * 16ll, left), f);
+    const gint* p = as_global((int*)place) + (size_t)token * a.choices;
+    const gfloat* pw = as_global(weights ? (float*)weights : (float*)place) + (size_t)token * a.choices;   // (read and not used without weights)
+    by_whole<V>(left, [&](auto whole) {
+        const int count = decltype(whole)::value ? V : left;
+        float sum[V] = {};
+        for (int k0 = 0; k0 < a.choices; k0 += GROUP) {
+            int row[GROUP];
+            float w[GROUP];
+            u4 r[GROUP];
 #pragma unroll
-        for (int j = 0; j < V; ++j) sum[j] = fmaf(w, f[j], sum[j]);
-    }
-    store_row16<ES>((gchar*)y + token * a.ld_token + c * 16ll, pack16<KIND>(sum), left);
+            for (int k = 0; k < GROUP; ++k) {
+                const int at = min(k0 + k, a.choices - 1);
+                row[k] = k0 + k < a.choices ? p[at] : -1;
+                w[k] = pw[at];
+            }
+#pragma unroll
+            for (int k = 0; k < GROUP; ++k)                         // (row 0 stands in for none)
+                r[k] = load_row16<ES, STREAM>((const gchar*)ys + ((unsigned)row[k] < (unsigned)a.rows ? row[k] : 0) * a.ld_row + c * 16ll, count);
+#pragma unroll
+            for (int k = 0; k < GROUP; ++k) {
+                float f[V];
+                unpack16<KIND>(r[k], f);
+                const bool there = (unsigned)row[k] < (unsigned)a.rows;
+                const float wk = weights ? w[k] : 1.f;
+#pragma unroll
+                for (int j = 0; j < V; ++j) sum[j] = there ? fmaf(wk, f[j], sum[j]) : sum[j];
+            }
+        }
+        store_row16<ES>((gchar*)y + token * a.ld_token + c * 16ll, pack16<KIND>(sum), count);
+    });
 }
 
-// One wavefront per token.
-template <int KIND>
+// WAVES wavefronts per token; dy's row is fetched once for every GROUP choices.
+template <int KIND, bool STREAM, int WAVES>
 __global__ __launch_bounds__(256) void expert_combine_backward_kernel(RowArgs a, int tokens, const char* dy, const char* ys, const float* weights,
                                                                       const int* place, char* dys, float* dweights) {
     constexpr int ES = elem_bytes<KIND>, V = elems16<KIND>;
-    const int lane = threadIdx.x & 63;
-    const unsigned token = blockIdx.x * 4u + (threadIdx.x >> 6);
-    if (token >= (unsigned)tokens) return;
+    __shared__ float red[GROUP][4];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned token = WAVES == 4 ? blockIdx.x : blockIdx.x * 4u + wave;
+    if (token >= (unsigned)tokens) return;                             // (WAVES = 4: never)
     const size_t at = (size_t)token * a.choices;
-    for (int k = 0; k < a.choices; ++k) {
-        const int row = place[at + k];
-        const bool there = (unsigned)row < (unsigned)a.rows;
-        float dot = 0.f;
-        if (there) {
-            const float w = weights ? weights[at + k] : 1.f;
-            for (unsigned c = lane; c < a.per_row; c += 64) {
-                const int left = a.dim - (int)c * V;
-                float g[V], f[V];
-                unpack16<KIND>(load_row16<ES>((const gchar*)dy + token * a.ld_token + c * 16ll, left), g);
-                if (dweights) {
-                    unpack16<KIND>(load_row16<ES>((const gchar*)ys + row * a.ld_row + c * 16ll, left), f);
+    for (int k0 = 0; k0 < a.choices; k0 += GROUP) {
+        int row[GROUP];
+        float w[GROUP], dot[GROUP];
 #pragma unroll
-                    for (int j = 0; j < V; ++j) dot = fmaf(g[j], f[j], dot);
+        for (int k = 0; k < GROUP; ++k) {
+            const int i = min(k0 + k, a.choices - 1);
+            const int r = place[at + i];
+            row[k] = __builtin_amdgcn_readfirstlane(k0 + k < a.choices && (unsigned)r < (unsigned)a.rows ? r : -1);
+            w[k] = weights ? weights[at + i] : 1.f;
+            dot[k] = 0.f;
+        }
+        for (unsigned c = WAVES == 4 ? threadIdx.x : lane; c < a.per_row; c += 64 * WAVES) {
+            const int left = a.dim - (int)c * V;
+            by_whole<V>(left, [&](auto whole) {
+                const int count = decltype(whole)::value ? V : left;
+                const u4 d = load_row16<ES>((const gchar*)dy + token * a.ld_token + c * 16ll, count);
+                u4 r[GROUP];
+                if (dweights) {                                        // (row 0 stands in for none)
+#pragma unroll
+                    for (int k = 0; k < GROUP; ++k) r[k] = load_row16<ES, STREAM>((const gchar*)ys + max(row[k], 0) * a.ld_row + c * 16ll, count);
+                }
+                float g[V], f[V];
+                unpack16<KIND>(d, g);
+                if (dweights) {
+#pragma unroll
+                    for (int k = 0; k < GROUP; ++k) {
+                        unpack16<KIND>(r[k], f);
+#pragma unroll
+                        for (int j = 0; j < V; ++j) dot[k] = fmaf(g[j], f[j], dot[k]);
+                    }
                 }
 #pragma unroll
-                for (int j = 0; j < V; ++j) g[j] *= w;
-                store_row16<ES>((gchar*)dys + row * a.ld_row + c * 16ll, pack16<KIND>(g), left);
-            }
+                for (int k = 0; k < GROUP; ++k) {
+                    if (row[k] < 0) continue;                          // (uniform)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) f[j] = g[j] * w[k];
+                    store_row16<ES, STREAM>((gchar*)dys + row[k] * a.ld_row + c * 16ll, pack16<KIND>(f), count);
+                }
+            });
         }
         if (dweights) {
 #pragma unroll
-            for (int off = 32; off > 0; off >>= 1) dot += __shfl_down(dot, off, 64);
-            if (lane == 0) dweights[at + k] = there ? dot : 0.f;
+            for (int k = 0; k < GROUP; ++k) {
+#pragma unroll
+                for (int off = 32; off > 0; off >>= 1) dot[k] += __shfl_down(dot[k], off, 64);
+                if (WAVES == 1 && lane == 0 && k0 + k < a.choices) dweights[at + k0 + k] = row[k] >= 0 ? dot[k] : 0.f;
+                if (WAVES == 4 && lane == 0) red[k][wave] = row[k] >= 0 ? dot[k] : 0.f;
+            }
+            if constexpr (WAVES == 4) {
+                const int k = threadIdx.x;
+                __syncthreads();
+                if (k < GROUP && k0 + k < a.choices) dweights[at + k0 + k] = (red[k][0] + red[k][1]) + (red[k][2] + red[k][3]);
+                __syncthreads();
+            }
         }
     }
 }
@@ -282,17 +399,23 @@ static bool rows_overlap(const void* p, long long np, long long ldp, const void*
 
 using namespace kfac;
 
-#define KFAC_BY_DTYPE(dtype, kernel, grid, block, stream, ...)                                     \
-    do {                                                                                          \
-        if ((dtype) == KFAC_BF16) KFAC_LAUNCH(kernel<0>, grid, block, stream, __VA_ARGS__);       \
-        else if ((dtype) == KFAC_F16) KFAC_LAUNCH(kernel<1>, grid, block, stream, __VA_ARGS__);   \
-        else KFAC_LAUNCH(kernel<2>, grid, block, stream, __VA_ARGS__);                            \
-    } while (0)
+// f(kind, streams): the constants of a dtype, and of a pass over `bytes` bytes.
+template <class F>
+static int by_type(int dtype, size_t bytes, F&& f) {
+    auto kind = [&](auto streams) -> int {
+        if (dtype == KFAC_BF16) return f(IntConstant<0>{}, streams);
+        if (dtype == KFAC_F16) return f(IntConstant<1>{}, streams);
+        return f(IntConstant<2>{}, streams);
+    };
+    return bytes > STREAM_BYTES ? kind(BoolConstant<true>{}) : kind(BoolConstant<false>{});
+}
+// Bytes of `token_rows` tensors in tokens' order and `sorted_rows` in the experts'.
+static size_t moved(const RowArgs& a, int token_rows, int sorted_rows) { return ((size_t)token_rows + (size_t)sorted_rows * a.choices) * a.vectors * 16; }
 
 extern "C" size_t kfac_expert_sort_workspace_bytes(const kfac_expert_desc* desc) {
     if (!route_ok(desc)) return 0;
     const SortCut c = sort_cut(desc->tokens * desc->choices, desc->experts);
-    return c.blocks > 1 ? align_up((size_t)c.blocks * desc->experts * sizeof(int), 256) : 0;
+    return c.blocks > 1 ? align_up((size_t)c.blocks * c.width * 16, 256) : 0;
 }
 
 extern "C" int kfac_expert_sort(const kfac_expert_desc* desc, const int32_t* expert, int32_t* offsets, int32_t* order, int32_t* place,
@@ -311,10 +434,14 @@ extern "C" int kfac_expert_sort(const kfac_expert_desc* desc, const int32_t* exp
     const SortCut c = sort_cut(n, E);
     hipStream_t st = (hipStream_t)stream;
     const int threads = 64 * c.waves;
-    if (c.blocks > 1) KFAC_LAUNCH(expert_count_kernel, dim3(c.blocks), dim3(threads), st, expert, n, E, c.waves * c.per_wave, (int*)ws);
+    if (c.blocks > 1) KFAC_LAUNCH(expert_count_kernel, dim3(c.blocks), dim3(threads), st, expert, n, E, c.waves * c.per_wave,
+                                  c.width, (uint16_t*)ws);
     void* tok = nullptr;
     if (timing_enabled()) timing_begin("expert_place_kernel", st, &tok);
-    hipLaunchKernelGGL(expert_place_kernel, dim3(c.blocks), dim3(threads), c.lds, st, expert, n, E, c.per_wave, c.bits, (const int*)ws, offsets,
+    auto kernel = c.per_wave <= 64 * SORT_STEPS        ? expert_place_kernel<SORT_STEPS>
+                  : c.per_wave <= 64 * SORT_STEPS_MANY ? expert_place_kernel<SORT_STEPS_MANY>
+                                                       : expert_place_kernel<0>;
+    hipLaunchKernelGGL(kernel, dim3(c.blocks), dim3(threads), c.lds, st, expert, n, E, c.per_wave, c.bits, c.width, (const uint16_t*)ws, offsets,
                        n > 0 ? order : nullptr, place);
     if (tok) timing_end(st, tok);
     KFAC_LAUNCH_CHECK();
@@ -328,10 +455,13 @@ extern "C" int kfac_expert_dispatch(const kfac_expert_desc* desc, const void* x,
     const int es = desc->dtype == KFAC_F32 ? 4 : 2;
     if (!on_grid(x, es) || !on_grid(xs, es) || !on_grid(place, 4)) return KFAC_ERR_INVALID_ARG;
     if (rows_overlap(x, desc->tokens, a.ld_token, xs, a.rows, a.ld_row, (long long)a.dim * es)) return KFAC_ERR_INVALID_ARG;
-    const dim3 grid((a.vectors + 255) / 256);
-    if (es == 4) KFAC_LAUNCH(expert_dispatch_kernel<4>, grid, dim3(256), (hipStream_t)stream, a, (const char*)x, place, (char*)xs);
-    else KFAC_LAUNCH(expert_dispatch_kernel<2>, grid, dim3(256), (hipStream_t)stream, a, (const char*)x, place, (char*)xs);
-    return KFAC_OK;
+    return by_type(desc->dtype, moved(a, 1, 1), [&](auto kind, auto streams) -> int {
+        constexpr int ES = elem_bytes<decltype(kind)::value>;
+        constexpr bool STREAM = decltype(streams)::value;
+        KFAC_LAUNCH_AS(STREAM ? "expert_dispatch_kernel<stream>" : "expert_dispatch_kernel", (expert_dispatch_kernel<ES, STREAM>),
+                       dim3((a.vectors + 255) / 256), dim3(256), (hipStream_t)stream, a, (const char*)x, place, (char*)xs);
+        return KFAC_OK;
+    });
 }
 
 extern "C" int kfac_expert_combine(const kfac_expert_desc* desc, const void* ys, const float* weights, const int32_t* place, void* y,
@@ -342,9 +472,12 @@ extern "C" int kfac_expert_combine(const kfac_expert_desc* desc, const void* ys,
     const int es = desc->dtype == KFAC_F32 ? 4 : 2;
     if (!on_grid(ys, es) || !on_grid(y, es) || !on_grid(place, 4) || (uintptr_t)weights % 4) return KFAC_ERR_INVALID_ARG;
     if (rows_overlap(y, desc->tokens, a.ld_token, ys, a.rows, a.ld_row, (long long)a.dim * es)) return KFAC_ERR_INVALID_ARG;
-    KFAC_BY_DTYPE(desc->dtype, expert_combine_kernel, dim3((a.vectors + 255) / 256), dim3(256), (hipStream_t)stream, a, (const char*)ys, weights,
-                  place, (char*)y);
-    return KFAC_OK;
+    return by_type(desc->dtype, moved(a, 1, 1), [&](auto kind, auto streams) -> int {
+        constexpr bool STREAM = decltype(streams)::value;
+        KFAC_LAUNCH_AS(STREAM ? "expert_combine_kernel<stream>" : "expert_combine_kernel", (expert_combine_kernel<decltype(kind)::value, STREAM>),
+                       dim3((a.vectors + 255) / 256), dim3(256), (hipStream_t)stream, a, (const char*)ys, weights, place, (char*)y);
+        return KFAC_OK;
+    });
 }
 
 extern "C" int kfac_expert_combine_backward(const kfac_expert_desc* desc, const void* dy, const void* ys, const float* weights,
@@ -358,7 +491,16 @@ extern "C" int kfac_expert_combine_backward(const kfac_expert_desc* desc, const 
     const long long row = (long long)a.dim * es;
     if (rows_overlap(dy, desc->tokens, a.ld_token, dys, a.rows, a.ld_row, row)) return KFAC_ERR_INVALID_ARG;
     if (dweights && rows_overlap(ys, a.rows, a.ld_row, dys, a.rows, a.ld_row, row)) return KFAC_ERR_INVALID_ARG;
-    KFAC_BY_DTYPE(desc->dtype, expert_combine_backward_kernel, dim3((desc->tokens + 3) / 4), dim3(256), (hipStream_t)stream, a, desc->tokens,
-                  (const char*)dy, (const char*)ys, weights, place, (char*)dys, dweights);
-    return KFAC_OK;
+    return by_type(desc->dtype, moved(a, 1, dweights ? 2 : 1), [&](auto kind, auto streams) -> int {
+        constexpr int KIND = decltype(kind)::value;
+        constexpr bool STREAM = decltype(streams)::value;
+        const char* name = STREAM ? "expert_combine_backward_kernel<stream>" : "expert_combine_backward_kernel";
+        if (a.per_row >= BACK_WORKGROUP || (desc->tokens <= BACK_FEW && a.per_row > 64))
+            KFAC_LAUNCH_AS(name, (expert_combine_backward_kernel<KIND, STREAM, 4>), dim3(desc->tokens), dim3(256), (hipStream_t)stream, a, desc->tokens,
+                           (const char*)dy, (const char*)ys, weights, place, (char*)dys, dweights);
+        else
+            KFAC_LAUNCH_AS(name, (expert_combine_backward_kernel<KIND, STREAM, 1>), dim3((desc->tokens + 3) / 4), dim3(256), (hipStream_t)stream, a,
+                           desc->tokens, (const char*)dy, (const char*)ys, weights, place, (char*)dys, dweights);
+        return KFAC_OK;
+    });
 }

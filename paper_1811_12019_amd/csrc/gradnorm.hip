@@ -9,37 +9,45 @@
 
 namespace kfac {
 
-constexpr int GN_MAX = 128;               // tensors per launch (an argument block of 3.7 KB)
+constexpr int GN_FEW = 64, GN_MAX = 512;  // tensors per launch (argument blocks of 1.9 and 15 KB)
 constexpr unsigned GN_CHUNK = 4096;       // elements
 constexpr int NORM_WGS = 1024;            // four workgroups to a CU
-constexpr int CLIP_WGS = 2048;
 
+template <int MAX>
 struct GradBatch {
     int count;
-    unsigned prefix[GN_MAX + 1];          // first chunk of tensor i
-    unsigned char dtype[GN_MAX];
-    unsigned long long n[GN_MAX];
-    const void* g[GN_MAX];
-    void* out[GN_MAX];
+    unsigned step;                        // chunks that a workgroup takes at a time
+    unsigned prefix[MAX + 1];             // first chunk of tensor i
+    unsigned char dtype[MAX];
+    unsigned long long n[MAX];
+    const void* g[MAX];
+    void* out[MAX];
 };
 
-// The workgroup's run of chunks, tensor by tensor: f(tensor, first element, behind the last one).
-template <class F>
-__device__ __forceinline__ void for_run(const GradBatch& b, F&& f) {
-    const int t = threadIdx.x;
-    const unsigned chunks = b.prefix[b.count];
-    const unsigned c0 = (unsigned)((unsigned long long)chunks * blockIdx.x / gridDim.x);
-    const unsigned c1 = (unsigned)((unsigned long long)chunks * (blockIdx.x + 1) / gridDim.x);
-    int m = __syncthreads_count(t < b.count - 1 && b.prefix[t + 1] <= c0);
-    for (; m < b.count && b.prefix[m] < c1; ++m) {
-        const unsigned first = b.prefix[m];
+// Chunks c0 .. c1 - 1, tensor by tensor from tensor m on, which is the first one's or an earlier one: f(tensor, first element, behind the last one).
+template <int MAX, class F>
+__device__ __forceinline__ void for_chunks(const GradBatch<MAX>& b, unsigned c0, unsigned c1, int& m, F&& f) {
+    while (b.prefix[m + 1] <= c0) ++m;
+    for (int k = m; k < b.count && b.prefix[k] < c1; ++k) {
+        const unsigned first = b.prefix[k];
         const unsigned long long from = c0 > first ? (unsigned long long)(c0 - first) * GN_CHUNK : 0;
-        const unsigned long long n = b.n[m], to = (unsigned long long)(c1 - first) * GN_CHUNK;
-        f(m, from, to < n ? to : n);
+        const unsigned long long n = b.n[k], to = (unsigned long long)(c1 - first) * GN_CHUNK;
+        f(k, from, to < n ? to : n);
     }
 }
+// The tensor of chunk c.
+template <int MAX>
+__device__ __forceinline__ int tensor_of(const GradBatch<MAX>& b, unsigned c) {
+    int m = 0;
+#pragma unroll
+    for (int k = 0; k < MAX; k += 256) {
+        const int i = threadIdx.x + k;
+        m += __syncthreads_count(i < b.count - 1 && b.prefix[min(i, MAX - 1) + 1] <= c);
+    }
+    return m;
+}
 
-template <int KIND>
+template <int KIND, bool STREAM>
 __device__ __forceinline__ double square_run(const gchar* g, unsigned long long count) {
     constexpr int V = elems16<KIND>, ES = elem_bytes<KIND>;
     const int t = threadIdx.x;
@@ -55,7 +63,7 @@ __device__ __forceinline__ double square_run(const gchar* g, unsigned long long 
     for (; v + 3 * 256 < vecs; v += 4 * 256) {
         u4 r[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) r[j] = load_row16<ES>(g + (v + j * 256) * 16, V);
+        for (int j = 0; j < 4; ++j) r[j] = load_row16<ES, STREAM>(g + (v + j * 256) * 16, V);
 #pragma unroll
         for (int j = 0; j < 4; ++j) add(r[j]);
     }
@@ -64,17 +72,25 @@ __device__ __forceinline__ double square_run(const gchar* g, unsigned long long 
     return s;
 }
 
-__global__ __launch_bounds__(256) void grad_partial_kernel(GradBatch b, double* partial) {
+template <bool STREAM>
+__device__ __forceinline__ double square_part(int dtype, const gchar* g, unsigned long long from, unsigned long long to) {
+    if (dtype == KFAC_F32) return square_run<2, STREAM>(g + from * 4, to - from);
+    if (dtype == KFAC_BF16) return square_run<0, STREAM>(g + from * 2, to - from);
+    return square_run<1, STREAM>(g + from * 2, to - from);
+}
+
+template <int MAX, bool STREAM>
+__global__ __launch_bounds__(256) void grad_partial_kernel(GradBatch<MAX> b, double* partial) {
     __shared__ double red[4];
     const int t = threadIdx.x;
+    const unsigned chunks = b.prefix[b.count];
+    int m = tensor_of(b, min(blockIdx.x * b.step, chunks - 1));
     double s = 0.0;
-    for_run(b, [&](int m, unsigned long long from, unsigned long long to) {
-        const gchar* g = (const gchar*)b.g[m];
-        const int dt = b.dtype[m];
-        if (dt == KFAC_F32) s += square_run<2>(g + from * 4, to - from);
-        else if (dt == KFAC_BF16) s += square_run<0>(g + from * 2, to - from);
-        else s += square_run<1>(g + from * 2, to - from);
-    });
+    for (unsigned long long c = (unsigned long long)blockIdx.x * b.step; c < chunks; c += (unsigned long long)gridDim.x * b.step)
+        for_chunks(b, (unsigned)c, min((unsigned)c + b.step, chunks), m, [&](int k, unsigned long long from, unsigned long long to) {
+            const gchar* g = (const gchar*)b.g[k];
+            s += square_part<STREAM>(b.dtype[k], g, from, to);
+        });
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) s += __shfl_down(s, off, 64);
     if ((t & 63) == 0) red[t >> 6] = s;
@@ -100,7 +116,7 @@ __global__ __launch_bounds__(256) void grad_norm_kernel(const double* partial, i
     if (threadIdx.x == 0) *norm = (float)sqrt(s);
 }
 
-template <int KIND>
+template <int KIND, bool STREAM>
 __device__ __forceinline__ void clip_run(const gchar* g, gchar* out, unsigned long long count, float scale) {
     constexpr int V = elems16<KIND>, ES = elem_bytes<KIND>;
     const int t = threadIdx.x;
@@ -116,15 +132,16 @@ __device__ __forceinline__ void clip_run(const gchar* g, gchar* out, unsigned lo
     for (; v + 3 * 256 < vecs; v += 4 * 256) {
         u4 r[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) r[j] = load_row16<ES>(g + (v + j * 256) * 16, V);
+        for (int j = 0; j < 4; ++j) r[j] = load_row16<ES, STREAM>(g + (v + j * 256) * 16, V);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) store_row16<ES>(out + (v + j * 256) * 16, scaled(r[j]), V);
+        for (int j = 0; j < 4; ++j) store_row16<ES, STREAM>(out + (v + j * 256) * 16, scaled(r[j]), V);
     }
     for (; v < vecs; v += 256) store_row16<ES>(out + v * 16, scaled(load_row16<ES>(g + v * 16, V)), V);
     if (t == 0 && count % V) store_row16<ES>(out + vecs * 16, scaled(load_row16<ES>(g + vecs * 16, (int)(count % V))), (int)(count % V));
 }
 
-__global__ __launch_bounds__(256) void grad_clip_kernel(GradBatch b, const double* partial, int n, const float* given, float max_norm, float* norm) {
+template <int MAX, bool STREAM>
+__global__ __launch_bounds__(256) void grad_clip_kernel(GradBatch<MAX> b, const double* partial, int n, const float* given, float max_norm, float* norm) {
     __shared__ double red[4];
     double len;
     if (given) {
@@ -134,14 +151,17 @@ __global__ __launch_bounds__(256) void grad_clip_kernel(GradBatch b, const doubl
         if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)len;
     }
     const float scale = len > (double)max_norm && len < __builtin_inf() ? (float)((double)max_norm / len) : 1.f;
-    for_run(b, [&](int m, unsigned long long from, unsigned long long to) {
-        const gchar* g = (const gchar*)b.g[m];
-        gchar* out = (gchar*)b.out[m];
+    const unsigned chunks = b.prefix[b.count];
+    const unsigned c0 = (gridDim.x - 1 - blockIdx.x) * b.step;           // (what the first pass read last comes first)
+    int m = tensor_of(b, c0);
+    for_chunks(b, c0, min(c0 + b.step, chunks), m, [&](int k, unsigned long long from, unsigned long long to) {
+        const gchar* g = (const gchar*)b.g[k];
+        gchar* out = (gchar*)b.out[k];
         if (scale == 1.f && g == out) return;
-        const int dt = b.dtype[m];
-        if (dt == KFAC_F32) clip_run<2>(g + from * 4, out + from * 4, to - from, scale);
-        else if (dt == KFAC_BF16) clip_run<0>(g + from * 2, out + from * 2, to - from, scale);
-        else clip_run<1>(g + from * 2, out + from * 2, to - from, scale);
+        const int dt = b.dtype[k];
+        if (dt == KFAC_F32) clip_run<2, STREAM>(g + from * 4, out + from * 4, to - from, scale);
+        else if (dt == KFAC_BF16) clip_run<0, STREAM>(g + from * 2, out + from * 2, to - from, scale);
+        else clip_run<1, STREAM>(g + from * 2, out + from * 2, to - from, scale);
     });
 }
 
@@ -162,12 +182,38 @@ static bool gn_total(const kfac_grad_item* items, int count, unsigned long long*
     return true;
 }
 
-// Launches: the next up to GN_MAX items that have elements, as a batch; returns its chunks (0: no more items).
-static unsigned gn_fill(const kfac_grad_item* items, int count, int* next, GradBatch* b) {
+// How the items that have elements are dealt to launches: f(first item, behind the last one, their number, their chunks).
+template <class F>
+static int gn_launches(const kfac_grad_item* items, int count, F&& f) {
+    for (int i = 0; i < count;) {
+        const int first = i;
+        unsigned chunks = 0;
+        int n = 0;
+        for (; i < count && n < GN_MAX; ++i) {
+            chunks += (unsigned)gn_chunks(items[i].n);
+            n += items[i].n != 0;
+        }
+        if (chunks) {
+            const int rc = f(first, i, n, chunks);
+            if (rc != KFAC_OK) return rc;
+        }
+    }
+    return KFAC_OK;
+}
+
+// Chunks to a step: one where that makes no more than 4096 workgroups, four (32 or 64 KB) of more, and as many as keep their number small.
+static unsigned gn_step(unsigned chunks) { return chunks <= 4096 ? 1 : chunks <= 4u << 20 ? 4 : (chunks >> 20); }
+static unsigned gn_steps(unsigned chunks) {
+    const unsigned step = gn_step(chunks);
+    return (unsigned)(((unsigned long long)chunks + step - 1) / step);
+}
+
+template <int MAX>
+static void gn_fill(const kfac_grad_item* items, int first, int last, GradBatch<MAX>* b) {
     b->count = 0;
     b->prefix[0] = 0;
-    for (; *next < count && b->count < GN_MAX; ++*next) {
-        const kfac_grad_item& it = items[*next];
+    for (int i = first; i < last; ++i) {
+        const kfac_grad_item& it = items[i];
         if (it.n == 0) continue;
         const int k = b->count++;
         b->prefix[k + 1] = b->prefix[k] + (unsigned)gn_chunks(it.n);
@@ -176,32 +222,20 @@ static unsigned gn_fill(const kfac_grad_item* items, int count, int* next, GradB
         b->g[k] = it.g;
         b->out[k] = it.out ? it.out : const_cast<void*>(it.g);
     }
-    return b->prefix[b->count];
+    b->step = gn_step(b->prefix[b->count]);
 }
 
-// Workgroups of a launch over `chunks` of `total` chunks, `wgs` for all of them.
-static unsigned gn_wgs(unsigned chunks, unsigned long long total, int wgs) {
-    unsigned long long n = total <= (unsigned long long)wgs ? chunks : ((unsigned long long)chunks * wgs + total - 1) / total;
-    return (unsigned)(n < chunks ? n : chunks);
+static size_t gn_bytes(const kfac_grad_item* items, int count) {
+    size_t bytes = 0;
+    for (int i = 0; i < count; ++i) bytes += (size_t)items[i].n * gn_elem_bytes(items[i].dtype);
+    return bytes;
 }
 
-// Workgroups, and doubles, of the first pass.
-static int gn_partials(const kfac_grad_item* items, int count, unsigned long long total) {
-    int n = 0;
-    unsigned chunks = 0;
-    int in_launch = 0;
-    for (int i = 0; i <= count; ++i) {
-        if (i == count || in_launch == GN_MAX) {
-            if (chunks) n += (int)gn_wgs(chunks, total, NORM_WGS);
-            chunks = 0;
-            in_launch = 0;
-            if (i == count) break;
-        }
-        if (items[i].n == 0) continue;
-        chunks += (unsigned)gn_chunks(items[i].n);
-        ++in_launch;
-    }
-    return n;
+// Workgroups, and sums, of the first pass's launch: all workgroups of the second one read them, at most 4096 of all launches.
+static unsigned norm_wgs(unsigned chunks, int count) {
+    const unsigned launches = (unsigned)((count + GN_MAX - 1) / GN_MAX), steps = gn_steps(chunks);
+    const unsigned most = launches <= 4 ? NORM_WGS : launches >= 64 ? 64 : 4096 / launches;
+    return steps < most ? steps : most;
 }
 
 static int gn_check(const kfac_grad_item* items, int32_t count, bool clip) {
@@ -222,15 +256,26 @@ static int gn_check(const kfac_grad_item* items, int32_t count, bool clip) {
     return gn_total(items, count, &total) ? KFAC_OK : KFAC_ERR_TOO_LARGE;
 }
 
-static int gn_first_pass(const kfac_grad_item* items, int count, unsigned long long total, double* partial, int* n, hipStream_t stream) {
-    GradBatch b;
+static int gn_first_pass(const kfac_grad_item* items, int count, double* partial, int* n, hipStream_t stream) {
     *n = 0;
-    for (int next = 0; unsigned chunks = gn_fill(items, count, &next, &b);) {
-        const unsigned wgs = gn_wgs(chunks, total, NORM_WGS);
-        KFAC_LAUNCH(grad_partial_kernel, dim3(wgs), dim3(256), stream, b, partial + *n);
+    const bool stream_pass = gn_bytes(items, count) > STREAM_BYTES;
+    return gn_launches(items, count, [&](int first, int last, int held, unsigned chunks) -> int {
+        const unsigned wgs = norm_wgs(chunks, count);
+        auto launch = [&](auto& b) -> int {
+            gn_fill(items, first, last, &b);
+            constexpr int MAX = sizeof(b.dtype);
+            if (stream_pass)
+                KFAC_LAUNCH_AS("grad_partial_kernel<stream>", (grad_partial_kernel<MAX, true>), dim3(wgs), dim3(256), stream, b, partial + *n);
+            else
+                KFAC_LAUNCH_AS("grad_partial_kernel", (grad_partial_kernel<MAX, false>), dim3(wgs), dim3(256), stream, b, partial + *n);
+            return KFAC_OK;
+        };
+        GradBatch<GN_FEW> few;
+        GradBatch<GN_MAX> many;
+        const int rc = held <= GN_FEW ? launch(few) : launch(many);
         *n += (int)wgs;
-    }
-    return KFAC_OK;
+        return rc;
+    });
 }
 
 }  // namespace kfac
@@ -240,7 +285,12 @@ using namespace kfac;
 extern "C" size_t kfac_grad_norm_workspace_bytes(const kfac_grad_item* items_host, int32_t count) {
     unsigned long long total;
     if (!items_host || count <= 0 || !gn_total(items_host, count, &total)) return 0;
-    return align_up((size_t)gn_partials(items_host, count, total) * sizeof(double), 256);
+    size_t n = 0;
+    gn_launches(items_host, count, [&](int, int, int, unsigned chunks) -> int {
+        n += norm_wgs(chunks, count);
+        return KFAC_OK;
+    });
+    return align_up(n * sizeof(double), 256);
 }
 
 extern "C" int kfac_grad_norm_batched(const kfac_grad_item* items_host, int32_t count, float* norm, void* ws, size_t ws_bytes, void* stream) {
@@ -251,7 +301,7 @@ extern "C" int kfac_grad_norm_batched(const kfac_grad_item* items_host, int32_t 
     gn_total(items_host, count, &total);
     if (total && (!ws || ((uintptr_t)ws & 255) || ws_bytes < kfac_grad_norm_workspace_bytes(items_host, count))) return KFAC_ERR_WORKSPACE;
     int n;
-    rc = gn_first_pass(items_host, count, total, (double*)ws, &n, (hipStream_t)stream);
+    rc = gn_first_pass(items_host, count, (double*)ws, &n, (hipStream_t)stream);
     if (rc != KFAC_OK) return rc;
     KFAC_LAUNCH(grad_norm_kernel, dim3(1), dim3(256), (hipStream_t)stream, (const double*)ws, n, norm);
     return KFAC_OK;
@@ -269,15 +319,28 @@ extern "C" int kfac_grad_clip_batched(const kfac_grad_item* items_host, int32_t 
     hipStream_t st = (hipStream_t)stream;
     int n = 0;
     if (!given_norm) {
-        rc = gn_first_pass(items_host, count, total, (double*)ws, &n, st);
+        rc = gn_first_pass(items_host, count, (double*)ws, &n, st);
         if (rc != KFAC_OK) return rc;
         if (!total) {                                          // no elements: a norm of 0
             KFAC_LAUNCH(grad_norm_kernel, dim3(1), dim3(256), st, (const double*)ws, 0, norm);
             return KFAC_OK;
         }
     }
-    GradBatch b;
-    for (int next = 0; unsigned chunks = gn_fill(items_host, count, &next, &b);)
-        KFAC_LAUNCH(grad_clip_kernel, dim3(gn_wgs(chunks, total, CLIP_WGS)), dim3(256), st, b, (const double*)ws, n, given_norm, max_norm, norm);
-    return KFAC_OK;
+    const bool stream_pass = 2 * gn_bytes(items_host, count) > STREAM_BYTES;
+    return gn_launches(items_host, count, [&](int first, int last, int held, unsigned chunks) -> int {
+        auto launch = [&](auto& b) -> int {
+            gn_fill(items_host, first, last, &b);
+            constexpr int MAX = sizeof(b.dtype);
+            if (stream_pass)
+                KFAC_LAUNCH_AS("grad_clip_kernel<stream>", (grad_clip_kernel<MAX, true>), dim3(gn_steps(chunks)), dim3(256), st, b, (const double*)ws, n,
+                               given_norm, max_norm, norm);
+            else
+                KFAC_LAUNCH_AS("grad_clip_kernel", (grad_clip_kernel<MAX, false>), dim3(gn_steps(chunks)), dim3(256), st, b, (const double*)ws, n,
+                               given_norm, max_norm, norm);
+            return KFAC_OK;
+        };
+        GradBatch<GN_FEW> few;
+        GradBatch<GN_MAX> many;
+        return held <= GN_FEW ? launch(few) : launch(many);
+    });
 }
