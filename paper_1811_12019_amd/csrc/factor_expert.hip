@@ -20,29 +20,48 @@ __global__ __launch_bounds__(256) void expert_pad_kernel(const char* x, const in
     *(KFAC_AS1 u4*)((gchar*)out + (size_t)i * 16) = load_row16<ES>((const gchar*)x + row * ld + c * 16ll, dim - (int)c * (16 / ES));
 }
 
-// One workgroup to a part of an expert of several ranges, as factor_tile_reduce_kernel's to a build's.
+// The parts (as factor_tile_reduce_kernel's workgroups take them) of the experts of several ranges, dealt to the launch's workgroups in runs: how
+// many there are is known here only.  (A workgroup for every part that there could be: 131,072 rows of 1,024 columns for 128 experts 185 us.)
 template <int GROUPS>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4, 8))) void expert_reduce_kernel(ExpertArgs a, int wgs_per) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4, 8))) void expert_reduce_kernel(ExpertArgs a, int per) {
     __shared__ __attribute__((aligned(16))) float lds[GROUPS == 1 ? 32 * 33 : RD_MANY_FLOATS];
-    const int j = blockIdx.x / wgs_per, local = blockIdx.x - j * wgs_per;
+    __shared__ int found[EXPERT_LDS_INTS];
     ExpertRange r;
-    if (!expert_range<true>(a, (int*)lds, [&](int) { return j; }, r)) return;
-    __syncthreads();                                                   // (the sums go where the range was found)
-    FactorPlan pl;
-    pl.tw = a.tw;
-    pl.tiles_dim = a.tiles_dim;
-    pl.ntiles = a.ntiles;
-    pl.nsplit = r.ranges;
-    pl.rows_per_split = a.rows_per;
-    pl.tile_floats = a.tile_floats;
-    pl.ws_bytes = 0;
-    Partial part;
-    part.tiles = as_global(a.tiles) + (size_t)r.part * a.ntiles * a.tile_floats;
-    part.sums = as_global(a.sums) + (size_t)r.part * (a.tiles_dim * a.tw);
-    reduce_partials<GROUPS>(expert_view(a, r.rows, r.rows), pl, part, expert_out(a, r.expert), expert_scale(a, r.rows), local, lds);
+    unsigned unit = 0, last = 0;
+    int j = 0;
+    bool there = expert_range<true>(a, found, [&](int all) {
+        const unsigned units = (unsigned)all * (unsigned)per, each = units / gridDim.x, more = units - each * gridDim.x;
+        unit = blockIdx.x * each + min(blockIdx.x, more);
+        last = unit + each + (blockIdx.x < more);
+        j = (int)(unit / (unsigned)per);
+        return unit < last ? j : -1;
+    }, r);
+    for (unsigned in = unit - (unsigned)j * (unsigned)per; unit < last; ++unit, ++in) {
+        if (in == (unsigned)per) {
+            in = 0;
+            ++j;
+            __syncthreads();
+            there = expert_range<true>(a, found, [&](int) { return j; }, r);
+        }
+        if (there) {
+            FactorPlan pl;
+            pl.tw = a.tw;
+            pl.tiles_dim = a.tiles_dim;
+            pl.ntiles = a.ntiles;
+            pl.nsplit = r.ranges;
+            pl.rows_per_split = a.rows_per;
+            pl.tile_floats = a.tile_floats;
+            pl.ws_bytes = 0;
+            Partial part;
+            part.tiles = as_global(a.tiles) + (size_t)r.part * a.ntiles * a.tile_floats;
+            part.sums = as_global(a.sums) + (size_t)r.part * (a.tiles_dim * a.tw);
+            reduce_partials<GROUPS>(expert_view(a, r.rows, r.rows), pl, part, expert_out(a, r.expert), expert_scale(a, r.rows), (int)in, lds);
+        }
+        __syncthreads();                                               // (the next part's sums go where these were)
+    }
 }
 
-constexpr int EXPERT_MAX = 1024;
+constexpr int EXPERT_MAX = 1024, REDUCE_WGS = 2048;
 constexpr long long EXPERT_LD_MAX = 1 << 18;   // elements: a range's bytes fit 32 bits
 
 struct ExpertCut {
@@ -59,6 +78,20 @@ static bool expert_factor_ok(const kfac_expert_factor_desc* d) {
            (d->packed == 0 || d->packed == 1) && (d->ld == 0 || (d->ld >= d->dim && d->ld <= (1ll << 28)));
 }
 
+// Width of the tiles and rows of a range, from the call's rows and experts of equal size.  Rows: as many as let all ranges run in as few rounds of the
+// workgroups that fit the chip (768, of 256-wide tiles 256, fp32 512 and one round more) as uncut experts would, counting half a range for every expert's
+// end, and not so few that a second range costs a tile more in partial sums than it saves; ranges near an average expert's rows are made longer, so that
+// most experts are one (three times as long where there are workgroups enough to even out the long ones); calls of few rows need no second launch.
+// Width: 64 where wider tiles would leave CUs without one, 256 from so many tile rows on that a workgroup outlasts its epilogue, with little padding.
+// Both sides, bf16, us (128- and 256-wide at the rows of a range that suit each best; 64- and 128-wide):
+//     512 columns, 8 experts of 4,096 rows 34 and 40; 32 of 1,024 39 and 46; 32 of 4,096 95 and 77; 128 of 1,024 98 and 94
+//     1,024 columns, 8 of 1,024 36 and 45; 8 of 4,096 78 and 69; 32 of 256 52 and 53; 32 of 1,024 105 and 93; 128 of 64 113 and 119; of 256 156 and 141
+//     2,048 columns, 8 of 256 40 and 48; 8 of 1,024 90 and 86; 32 of 64 115 and 118; 32 of 256 168 and 147; 32 of 1,024 345 and 257
+//     512 columns, 8 experts of 64 rows 8.3 and 10.4; of 256 10.3 and 12.4; 32 of 64 15.9 and 13.2; fp32, 256 columns, 8 of 256 16 and 21; 8 of 2,048 32 and 30
+// Rows of a range: 1,024 columns, 256 wide, 32 of 4,096 1,024 298, 2,048 246, 6,400 211; 8 of 4,096 86, 69, 111; 512 columns, 128 wide, 8 of 4,096
+// 1,024 36, 1,536 34, 3,072 46; fp32, 1,024 columns, 8 of 1,024 256 108, 512 100, 1,024 118; 512 columns, 64 of 1,024 512 195, 1,024 200, 1,600 213.
+constexpr double FEW_WGS = 160, WIDE_TILE_ROWS = 200000;
+
 static ExpertCut expert_cut(const kfac_expert_factor_desc& d) {
     ExpertCut c;
     const bool f32 = d.dtype == KFAC_F32;
@@ -67,21 +100,19 @@ static ExpertCut expert_cut(const kfac_expert_factor_desc& d) {
     c.pad = ld % V != 0 || ld > EXPERT_LD_MAX;
     c.ld = c.pad ? (d.dim + V - 1) / V * V : (int)ld;
     c.pad_bytes = c.pad ? align_up((size_t)d.rows * c.ld * (f32 ? 4 : 2), 256) : 0;
-    // The work as a call of the other builders counts it, with equal experts (factor_cut.h).
-    TileWork w;
-    const double n = ceil_div(d.dim, 128), m = ceil_div(d.dim, 256), rows = d.rows;
-    w.narrow = 0.5 * n * (n + 1) * rows;
-    w.wide = d.dim <= 128 ? w.narrow : 2.0 * m * (m + 1) * rows;
-    c.rows_per = (rows_of(w, f32) + 63) / 64 * 64;
-    if (d.dim > 128) {
-        w.over = w.narrow;
-        w.area = 256.0 * m * 256.0 * m * rows;
-        w.filled = (double)d.dim * d.dim * rows;
-        const double tiles = 0.5 * m * (m + 1), each = rows / d.experts;
-        w.wide_rows = tiles * rows;
-        w.wide_wgs = (int)std::min(1e9, tiles * d.experts * std::max(1.0, std::ceil(each / c.rows_per)));
-    }
-    c.tw = d.dim <= 64 ? 64 : d.dim <= 128 || f32 || !takes_wide(w, c.rows_per) ? 128 : 256;
+    const double rows = d.rows, each = rows / d.experts;
+    auto tiles = [&](int tw) { const double n = ceil_div(d.dim, tw); return 0.5 * n * (n + 1); };
+    auto rows_of_width = [&](int tw) {
+        const double slots = tw == 256 ? 256 : f32 ? 512 : 768, whole = tiles(tw) * d.experts, rounds = std::max(std::ceil(whole / slots), 1.0) + f32;
+        double r = std::max(rows * tiles(tw) / (0.95 * rounds * slots - 0.5 * whole), !f32 ? 1024.0 : tw == 64 ? 128.0 : 256.0);
+        if (!f32 && r > 0.6 * each) r = std::max(r, (whole >= 2 * slots ? 3 : 1.5) * each);
+        if (rows <= (f32 ? 1024 : 2048) && (tw == 64 || !f32)) r = std::max(r, rows);
+        return (int)(std::min(r, (double)(f32 ? ROWS_PER_WG_MAX_F32 : ROWS_PER_WG_MAX)) + 63) / 64 * 64;
+    };
+    c.tw = 128;
+    if (d.dim <= 64 || tiles(128) * d.experts * std::max(1.0, std::ceil(each / rows_of_width(128))) < FEW_WGS) c.tw = 64;
+    else if (!f32 && d.dim > 128 && 4 * tiles(256) <= WIDE_PADDING * tiles(128) && tiles(256) * rows >= WIDE_TILE_ROWS) c.tw = 256;
+    c.rows_per = rows_of_width(c.tw);
     c.tiles_dim = ceil_div(d.dim, c.tw);
     c.ntiles = c.tiles_dim * (c.tiles_dim + 1) / 2;
     c.tile_floats = tile_floats(c.tw, c.ntiles);
@@ -143,13 +174,15 @@ extern "C" int kfac_expert_factor(const kfac_expert_factor_desc* desc, const voi
     a.ranges = (int)c.ranges;
     a.parts = (int)c.parts;
     const long long wgs = (c.ranges * c.ntiles + 7) / 8 * 8;
-    const int groups = ceil_div(d.rows, c.rows_per) >= MANY_SPLITS ? 4 : 1;
-    const int wgs_per = c.ntiles * (c.tw / 32) * (c.tw / 32) * groups + (d.has_bias ? ceil_div(d.dim, 256) : 0);
-    const long long reduce_wgs = c.splits * wgs_per;
+    // (Four workgroups to a part, which share out its rows and its sums, where there are many ranges to an expert and few parts: 64 columns, 4 experts
+    // of 16 ranges 15.0 -> 13.4 us, 192 columns, 2 of 10 16.5 -> 14.9; 256 columns, 8 of 8, 384 parts, 23.8 and 26.8.)
+    const int groups = d.rows / d.experts >= 4 * c.rows_per && (long long)d.experts * c.ntiles * (c.tw / 32) * (c.tw / 32) <= 256 ? 4 : 1;
+    const long long wgs_per = (long long)c.ntiles * (c.tw / 32) * (c.tw / 32) * groups + (d.has_bias ? ceil_div(d.dim, 256) : 0);
+    const long long reduce_wgs = std::min(c.splits * wgs_per, (long long)REDUCE_WGS);
     const int V = f32 ? 4 : 8;
     const long long vectors = c.pad ? (long long)d.rows * (c.ld / V) : 0;
     // (a launch has fewer than 2^32 threads)
-    if (wgs * (c.tw == 256 ? 512 : 256) >= 1ll << 32 || reduce_wgs * 256 >= 1ll << 32 || vectors > 0x7fffffffll) return KFAC_ERR_TOO_LARGE;
+    if (wgs * (c.tw == 256 ? 512 : 256) >= 1ll << 32 || c.splits * wgs_per >= 1ll << 32 || vectors > 0x7fffffffll) return KFAC_ERR_TOO_LARGE;
     if (vectors) {
         const dim3 grid((unsigned)((vectors + 255) / 256));
         const long long ld = (d.ld ? d.ld : d.dim) * es;
@@ -163,8 +196,8 @@ extern "C" int kfac_expert_factor(const kfac_expert_factor_desc* desc, const voi
                                        : launch_expert_tiles<2>(a, (unsigned)wgs, st);
     if (rc != KFAC_OK) return rc;
     if (reduce_wgs) {
-        if (groups == 4) KFAC_LAUNCH(expert_reduce_kernel<4>, dim3((unsigned)reduce_wgs), dim3(256), st, a, wgs_per);
-        else KFAC_LAUNCH(expert_reduce_kernel<1>, dim3((unsigned)reduce_wgs), dim3(256), st, a, wgs_per);
+        if (groups == 4) KFAC_LAUNCH(expert_reduce_kernel<4>, dim3((unsigned)reduce_wgs), dim3(256), st, a, (int)wgs_per);
+        else KFAC_LAUNCH(expert_reduce_kernel<1>, dim3((unsigned)reduce_wgs), dim3(256), st, a, (int)wgs_per);
     }
     return KFAC_OK;
 }
