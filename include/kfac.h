@@ -231,7 +231,8 @@ typedef struct kfac_expert_desc {
     int32_t dim;         /* D: elements of a token's row, 1 .. 2^20 (not used by kfac_expert_sort) */
     int32_t dtype;       /* kfac_dtype of the rows (not used by kfac_expert_sort) */
     int64_t ld_token;    /* elements from one row to the next of tensors in tokens' order (x, y, dy); 0: D */
-    int64_t ld_row;      /* the same of tensors in the experts' order (xs, ys, dys), of T K rows; 0: D */
+    int64_t ld_row;      /* the same of tensors in the experts' order (xs, ys), of T K rows; 0: D */
+    int64_t ld_grad;     /* the same of dys; 0: D */
 } kfac_expert_desc;
 
 /* expert: T x K int32.  Assignment i = t K + k goes to row place[i]; expert e's rows are offsets[e] .. offsets[e + 1] - 1, with its

@@ -87,7 +87,7 @@ class kfac_grad_item(ctypes.Structure):
 
 class kfac_expert_desc(ctypes.Structure):
     _fields_ = ([(n, ctypes.c_int32) for n in ("tokens", "choices", "experts", "dim", "dtype")] +
-                [("ld_token", ctypes.c_int64), ("ld_row", ctypes.c_int64)])
+                [(n, ctypes.c_int64) for n in ("ld_token", "ld_row", "ld_grad")])
 
 
 class kfac_expert_factor_desc(ctypes.Structure):
@@ -548,7 +548,7 @@ class ExpertRoute:
         self.device = _gpu(device, "ExpertRoute")
         self.index = self.device.index
         self.tokens, self.choices, self.experts = int(tokens), int(choices), int(experts)
-        self.desc = kfac_expert_desc(self.tokens, self.choices, self.experts, 0, 0, 0, 0)
+        self.desc = kfac_expert_desc(self.tokens, self.choices, self.experts, 0, 0, 0, 0, 0)
         rows = self.tokens * self.choices
         _want(self.tokens >= 0 and self.choices >= 1 and self.experts >= 1, "ExpertRoute", "tokens, choices, experts")
         i32 = dict(dtype=torch.int32, device=self.device)
@@ -570,20 +570,20 @@ class ExpertRoute:
         _want(rows <= 1 or t.stride(0) >= t.shape[1], where, f"{name}: rows apart from each other")
         return 0 if rows <= 1 else t.stride(0)
 
-    def _rows(self, where, token_side, *row_side):
-        """The descriptor of a call on these tensors."""
+    def _rows(self, where, token_side, row_side, grad_side=None):
+        """The descriptor of a call on these tensors: one in tokens' order, one or none in the experts', the gradient of such a one or none."""
         key = (token_side.shape, token_side.stride(), token_side.dtype, token_side.get_device())
-        for t in row_side:
-            key += (t.shape, t.stride(), t.dtype, t.get_device())
+        for t in (row_side, grad_side):
+            key += (None,) if t is None else (t.shape, t.stride(), t.dtype, t.get_device())
         desc = self._descs.get(key)
         if desc is None:
             rows = self.tokens * self.choices
-            ld_token = self._side(token_side, self.tokens, where, "a tensor in tokens' order")
-            ld = [self._side(t, rows, where, "a tensor in the experts' order") for t in row_side]
-            _want(all(t.shape[1] == token_side.shape[1] and t.dtype == token_side.dtype for t in row_side), where, "rows of one width and type")
-            _want(len(set(ld)) == 1, where, "the same stride for both tensors in the experts' order")
+            ld = [self._side(token_side, self.tokens, where, "a tensor in tokens' order")]
+            for t in (row_side, grad_side):
+                ld.append(0 if t is None else self._side(t, rows, where, "a tensor in the experts' order"))
+                _want(t is None or (t.shape[1] == token_side.shape[1] and t.dtype == token_side.dtype), where, "rows of one width and type")
             desc = self._descs[key] = ctypes.byref(kfac_expert_desc(self.tokens, self.choices, self.experts, token_side.shape[1],
-                                                                    _KFAC_DTYPE[token_side.dtype], ld_token, ld[0]))
+                                                                    _KFAC_DTYPE[token_side.dtype], *ld))
         return desc
 
     def _weights(self, t, where, name):
@@ -628,7 +628,7 @@ def kfac_expert_combine_backward(route: ExpertRoute, dy: torch.Tensor, ys: Optio
     """dy: (T, D), ys and dys: (T K, D), weights and dweights: (T, K) float32.  dweights = None: ys is not read and may be None."""
     where = "kfac_expert_combine_backward"
     _want(dweights is None or ys is not None, where, "dweights needs ys")
-    desc = route._rows(where, dy, dys) if dweights is None else route._rows(where, dy, dys, ys)
+    desc = route._rows(where, dy, None if dweights is None else ys, dys)
     rc = load_library().kfac_expert_combine_backward(desc, dy.data_ptr(), None if dweights is None else ys.data_ptr(),
                                                      route._weights(weights, where, "weights"), route.place.data_ptr(), dys.data_ptr(),
                                                      route._weights(dweights, where, "dweights"), _stream_on(route.index, where, stream))

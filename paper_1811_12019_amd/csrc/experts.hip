@@ -222,7 +222,7 @@ __global__ __launch_bounds__(1024) void expert_place_kernel(const int* expert, i
 struct RowArgs {
     unsigned vectors, per_row;
     int choices, rows, dim;
-    long long ld_token, ld_row;           // bytes
+    long long ld_token, ld_row, ld_grad;  // bytes
 };
 
 // The last vector of a row may hold fewer elements than the others: f(true) where it does not, so that the loads of f can all be on their way at
@@ -339,7 +339,7 @@ __global__ __launch_bounds__(256) void expert_combine_backward_kernel(RowArgs a,
                     if (row[k] < 0) continue;                          // (uniform)
 #pragma unroll
                     for (int j = 0; j < V; ++j) f[j] = g[j] * w[k];
-                    store_row16<ES, STREAM>((gchar*)dys + row[k] * a.ld_row + c * 16ll, pack16<KIND>(f), count);
+                    store_row16<ES, STREAM>((gchar*)dys + row[k] * a.ld_grad + c * 16ll, pack16<KIND>(f), count);
                 }
             });
         }
@@ -371,8 +371,9 @@ static int row_args(const kfac_expert_desc* d, RowArgs* a) {
     if (!route_ok(d) || d->dim < 1 || d->dim > EX_MAX_DIM) return KFAC_ERR_INVALID_ARG;
     if (d->dtype != KFAC_F32 && d->dtype != KFAC_BF16 && d->dtype != KFAC_F16) return KFAC_ERR_INVALID_ARG;
     const int es = d->dtype == KFAC_F32 ? 4 : 2;
-    const long long lt = d->ld_token ? d->ld_token : d->dim, lr = d->ld_row ? d->ld_row : d->dim;
-    if (lt < d->dim || lr < d->dim || lt > (1ll << 28) || lr > (1ll << 28)) return KFAC_ERR_INVALID_ARG;
+    const long long lt = d->ld_token ? d->ld_token : d->dim, lr = d->ld_row ? d->ld_row : d->dim, lg = d->ld_grad ? d->ld_grad : d->dim;
+    for (long long ld : {lt, lr, lg})
+        if (ld < d->dim || ld > (1ll << 28)) return KFAC_ERR_INVALID_ARG;
     a->per_row = (unsigned)(((long long)d->dim * es + 15) / 16);
     const unsigned long long vectors = (unsigned long long)d->tokens * a->per_row;
     if (vectors > 0x7fffffffull) return KFAC_ERR_TOO_LARGE;
@@ -382,6 +383,7 @@ static int row_args(const kfac_expert_desc* d, RowArgs* a) {
     a->dim = d->dim;
     a->ld_token = lt * es;
     a->ld_row = lr * es;
+    a->ld_grad = lg * es;
     return KFAC_OK;
 }
 
@@ -489,8 +491,8 @@ extern "C" int kfac_expert_combine_backward(const kfac_expert_desc* desc, const 
     if (!on_grid(dy, es) || !on_grid(dys, es) || !on_grid(place, 4) || (uintptr_t)weights % 4 || (uintptr_t)dweights % 4) return KFAC_ERR_INVALID_ARG;
     if (dweights && !on_grid(ys, es)) return KFAC_ERR_INVALID_ARG;
     const long long row = (long long)a.dim * es;
-    if (rows_overlap(dy, desc->tokens, a.ld_token, dys, a.rows, a.ld_row, row)) return KFAC_ERR_INVALID_ARG;
-    if (dweights && rows_overlap(ys, a.rows, a.ld_row, dys, a.rows, a.ld_row, row)) return KFAC_ERR_INVALID_ARG;
+    if (rows_overlap(dy, desc->tokens, a.ld_token, dys, a.rows, a.ld_grad, row)) return KFAC_ERR_INVALID_ARG;
+    if (dweights && rows_overlap(ys, a.rows, a.ld_row, dys, a.rows, a.ld_grad, row)) return KFAC_ERR_INVALID_ARG;
     return by_type(desc->dtype, moved(a, 1, dweights ? 2 : 1), [&](auto kind, auto streams) -> int {
         constexpr int KIND = decltype(kind)::value;
         constexpr bool STREAM = decltype(streams)::value;

@@ -231,6 +231,72 @@ class KfacNetworkStep:
             l.G_run.copy_(torch.eye(l.shape.d_G, device=l.G_run.device))
 
 
+class KfacExpertStep:
+    """One layer of experts resident on one GPU: each of `tokens` tokens goes to `choices` of `experts` linear maps of d_in to d_out
+    features.  Every expert has Kronecker factors of its own, from the tokens that came to it; which ones these are is decided on
+    the device, and nothing here waits for the host.
+
+        xs = layer.dispatch(expert, x)                   tokens in the experts' order: rows offsets[e] .. offsets[e + 1] - 1 are expert e's
+        y = layer.combine(ys, weights)                   ys[r] = W_e xs[r], the caller's products
+        dys, dweights = layer.backward(dy, ys, weights)  gradients of the experts' outputs and of the weights
+        dx = layer.input_gradient(dxs)                   dxs[r] = W_e^T dys[r]
+        P = layer.step()                                 factors, running averages, inverses, preconditioned gradients of layer.gradW
+
+    gradW (experts, d_out, d_in) is the caller's to fill; step() clips P by the norm over all experts if max_norm is given (layer.norm is that
+    norm).  The running averages of an expert without tokens stay as they are."""
+
+    def __init__(self, tokens: int, choices: int, experts: int, d_in: int, d_out: int, dtype: torch.dtype = torch.bfloat16, decay: float = 0.95,
+                 gamma: float = 1e-3, max_norm: Optional[float] = None, device="cuda"):
+        self.decay, self.max_norm = float(decay), max_norm
+        self.route = kb.ExpertRoute(tokens, choices, experts, device=device)
+        device = self.route.device
+        rows = tokens * choices
+        f32 = dict(dtype=torch.float32, device=device)
+        # rows of whole 16-byte vectors, which the factors' builders read as they lie
+        def rows_of(dim):
+            vector = 4 if dtype == torch.float32 else 8
+            return torch.zeros((rows, -(-dim // vector) * vector), dtype=dtype, device=device)[:, :dim]
+
+        self.xs, self.dys = rows_of(d_in), rows_of(d_out)
+        self.y, self.dx = (torch.empty((tokens, d), dtype=dtype, device=device) for d in (d_out, d_in))
+        self.dweights = torch.empty((tokens, choices), **f32)
+        self.A_plan, self.G_plan = (kb.ExpertFactors(rows, experts, t.shape[1], dtype, ld=t.stride(0), device=device) for t in (self.xs, self.dys))
+        self.A_run, self.G_run = (torch.eye(d, **f32).repeat(experts, 1, 1) for d in (d_in, d_out))
+        self.A_inv, self.G_inv = torch.empty_like(self.A_run), torch.empty_like(self.G_run)
+        self.gradW, self.P = (torch.zeros((experts, d_out, d_in), **f32) for _ in range(2))
+        src, dst = [*self.A_run, *self.G_run], [*self.A_inv, *self.G_inv]
+        planes = [kb.alloc_workspace(kb.kfac_inverse_planes_bytes(t.shape[0]), device) for t in src]
+        self.inverses = kb.InverseBatch(src, dst, [float(gamma) ** 0.5] * len(src), device=device, planes=planes)
+        self.precond = kb.PrecondBatch([*self.G_inv], [*self.A_inv], [*self.gradW], [*self.P], device=device, Ginv_planes=planes[experts:],
+                                       Ainv_planes=planes[:experts])
+        self.clip = None if max_norm is None else kb.GradBatch([self.P], device=device)
+        self.norm = None if self.clip is None else self.clip.norm
+
+    def dispatch(self, expert: torch.Tensor, x: torch.Tensor, stream=None) -> torch.Tensor:
+        kb.kfac_expert_sort(self.route, expert, stream)
+        return kb.kfac_expert_dispatch(self.route, x, self.xs, stream)
+
+    def combine(self, ys: torch.Tensor, weights: torch.Tensor, stream=None) -> torch.Tensor:
+        return kb.kfac_expert_combine(self.route, ys, weights, self.y, stream)
+
+    def backward(self, dy: torch.Tensor, ys: torch.Tensor, weights: torch.Tensor, stream=None):
+        kb.kfac_expert_combine_backward(self.route, dy, ys, weights, self.dys, self.dweights, stream)
+        return self.dys, self.dweights
+
+    def input_gradient(self, dxs: torch.Tensor, stream=None) -> torch.Tensor:
+        return kb.kfac_expert_combine(self.route, dxs, None, self.dx, stream)
+
+    def step(self, refresh_inverse: bool = True, stream=None) -> torch.Tensor:
+        kb.kfac_expert_factor(self.A_plan, self.xs, self.route.offsets, running=self.A_run, decay=self.decay, stream=stream)
+        kb.kfac_expert_factor(self.G_plan, self.dys, self.route.offsets, running=self.G_run, decay=self.decay, stream=stream)
+        if refresh_inverse:
+            kb.kfac_damped_inverse_batched(self.inverses, stream)
+        kb.kfac_precondition_batched(self.precond, stream)
+        if self.clip is not None:
+            kb.kfac_grad_clip_batched(self.clip, self.max_norm, stream=stream)
+        return self.P
+
+
 # Algorithmic work, for rooflines (2 flops per multiply-add; symmetric outputs counted as a triangle).
 def factor_flops(rows: int, dim: int) -> float:
     return float(rows) * dim * (dim + 1)

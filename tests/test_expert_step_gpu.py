@@ -1,0 +1,135 @@
+"""A layer of experts from routing to the weights' update, every stage against the float64 oracle on the GPU's own input to it.
+
+Tolerances: rows as in tests/test_experts_gpu.py; running averages 2e-5 (their fresh part's) of the Frobenius norm; inverses and preconditioned
+gradients 1e-4, clipped values 2^-22, weights 3e-6 of the largest, as in tests/test_parity_gpu.py and tests/test_grad_clip_gpu.py."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import experts_oracle as eo
+from oracle import kfac_oracle as ko
+from paper_1811_12019_amd import binding as kb
+from paper_1811_12019_amd.step import KfacExpertStep
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def near(got, want, tol):
+    got, want = f64(got), np.asarray(want)
+    assert np.linalg.norm(got - want) <= tol * np.linalg.norm(want)
+
+
+def tokens(T, K, E, d_in, d_out, dtype, seed):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    expert = torch.randint(0, E - 1, (T, K), generator=g, device=DEV, dtype=torch.int32)      # the last expert gets none
+    expert[torch.rand((T, K), generator=g, device=DEV) < 0.1] = -1
+    x = torch.randn((T, d_in), generator=g, device=DEV).relu().to(dtype)
+    weights = torch.rand((T, K), generator=g, device=DEV)
+    dy = (torch.randn((T, d_out), generator=g, device=DEV) * 0.1).to(dtype)
+    return expert, x, weights, dy
+
+
+def experts_products(layer, W, xs):
+    """ys[r] = W_e xs[r], and the gradient of W_e from the layer's dys: the caller's part, in plain torch."""
+    cut = layer.route.offsets.tolist()
+    ys = torch.zeros((xs.shape[0], W.shape[1]), dtype=xs.dtype, device=DEV)
+    for e, (a, b) in enumerate(zip(cut, cut[1:])):
+        ys[a:b] = (xs[a:b].float() @ W[e].t()).to(xs.dtype)
+    return ys, cut
+
+
+@pytest.mark.parametrize("T,K,E,d_in,d_out,dtype", [(300, 2, 5, 40, 24, torch.bfloat16), (150, 3, 4, 33, 130, torch.float32), (64, 1, 3, 16, 7, torch.float16)])
+def test_steps_of_a_layer_of_experts(T, K, E, d_in, d_out, dtype):
+    decay, gamma, max_norm, eta, momentum = 0.9, 1e-2, 0.5, 0.05, 0.9
+    layer = KfacExpertStep(T, K, E, d_in, d_out, dtype, decay, gamma, max_norm)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    W = torch.randn((E, d_out, d_in), generator=g, device=DEV) * 0.2
+    W_prev = W.clone()
+    update = kb.UpdateBatch([*W], [*W_prev], [*layer.P])
+    half = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11, torch.float32: 2.0 ** -24}[dtype]
+    A, G = f64(layer.A_run), f64(layer.G_run)
+    for seed in (1, 2):
+        expert, x, weights, dy = tokens(T, K, E, d_in, d_out, dtype, seed)
+        xs = layer.dispatch(expert, x)
+        offsets, order, place = eo.expert_sort(expert.cpu().numpy(), E)
+        np.testing.assert_array_equal(layer.route.offsets.cpu().numpy(), offsets)
+        rows = offsets[-1]
+        np.testing.assert_array_equal(f64(xs)[:rows], eo.expert_dispatch(f64(x), place, np.zeros((T * K, d_in)))[:rows])
+        ys, cut = experts_products(layer, W, xs)
+        y = layer.combine(ys, weights)
+        near(y, eo.expert_combine(f64(ys), f64(weights), place, d_out), 2 * half + K * 2.0 ** -24)
+        dys, dweights = layer.backward(dy, ys, weights)
+        want_dys, want_dw = eo.expert_combine_backward(f64(dy), f64(ys), f64(weights), place, np.zeros((T * K, d_out)))
+        assert np.linalg.norm(f64(dys)[:rows] - want_dys[:rows]) <= 2 * half * np.linalg.norm(want_dys)
+        near(dweights, want_dw, 1e-5)
+        dxs = torch.zeros((T * K, d_in), dtype=dtype, device=DEV)
+        for e in range(E):
+            a, b = cut[e], cut[e + 1]
+            dxs[a:b] = (dys[a:b].float() @ W[e]).to(dtype)
+            layer.gradW[e] = dys[a:b].float().t() @ xs[a:b].float()
+        near(layer.input_gradient(dxs), eo.expert_combine(f64(dxs), None, place, d_in), 2 * half + K * 2.0 ** -24)
+        P = layer.step()
+        assert layer.inverses.info.tolist() == [0] * (2 * E)
+        A, G = (eo.expert_factor(f64(t), offsets, running=S, decay=decay) for t, S in ((xs, A), (dys, G)))
+        near(layer.A_run, A, 2e-5)
+        near(layer.G_run, G, 2e-5)
+        A, G = f64(layer.A_run), f64(layer.G_run)
+        assert np.array_equal(A[-1], np.eye(d_in)) and np.array_equal(G[-1], np.eye(d_out))
+        lam = float(np.float32(gamma ** 0.5))
+        want = []
+        for e in range(E):
+            near(layer.A_inv[e], np.linalg.inv(A[e] + lam * np.eye(d_in)), 1e-4)
+            near(layer.G_inv[e], np.linalg.inv(G[e] + lam * np.eye(d_out)), 1e-4)
+            want.append(f64(layer.G_inv[e]) @ f64(layer.gradW[e]) @ f64(layer.A_inv[e]))
+        want, norm = eo.grad_clip([np.stack(want)], max_norm)
+        assert norm > max_norm
+        assert abs(float(layer.norm) - norm) <= 1e-4 * norm
+        near(P, want[0], 2e-4)
+        assert abs(np.linalg.norm(f64(P)) - max_norm) <= 2.0 ** -22 * max_norm
+        before, before_prev, p = f64(W), f64(W_prev), f64(P)
+        kb.kfac_weight_update_batched(update, eta, momentum)
+        for e in range(E):
+            new = ko.rescale_weights(ko.weight_update(before[e], before_prev[e], p[e], eta, momentum), d_out)
+            assert np.abs(f64(W[e]) - new).max() <= 3e-6 * np.abs(new).max()
+        np.testing.assert_array_equal(f64(W_prev), before)
+    stale = layer.A_inv.clone()
+    layer.step(refresh_inverse=False)
+    assert torch.equal(layer.A_inv, stale)
+
+
+def test_a_captured_layer():
+    """The calls between the caller's products, captured once and replayed on other tokens, against eager calls."""
+    T, K, E, d_in, d_out, dtype = 500, 2, 6, 64, 48, torch.bfloat16
+    one, two = (KfacExpertStep(T, K, E, d_in, d_out, dtype, max_norm=1.0) for _ in range(2))
+    held = [t.clone() for t in tokens(T, K, E, d_in, d_out, dtype, 0)]
+    ys = torch.zeros((T * K, d_out), dtype=dtype, device=DEV)
+
+    def calls(layer):
+        layer.dispatch(held[0], held[1])
+        layer.combine(ys, held[2])
+        layer.backward(held[3], ys, held[2])
+        layer.step()
+
+    calls(one)
+    calls(two)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls(one)
+    for seed in range(1, 5):
+        for t, new in zip(held, tokens(T, K, E, d_in, d_out, dtype, seed)):
+            t.copy_(new)
+        g = torch.Generator(device=DEV).manual_seed(seed)
+        ys.copy_(torch.randn(ys.shape, generator=g, device=DEV))
+        for layer in (one, two):
+            layer.gradW.copy_(torch.randn(layer.gradW.shape, generator=g, device=DEV) if layer is one else one.gradW)
+        graph.replay()
+        calls(two)
+        torch.cuda.synchronize()
+        for name in ("xs", "y", "dys", "dweights", "A_run", "G_run", "A_inv", "P", "norm"):
+            assert torch.equal(getattr(one, name), getattr(two, name)), (seed, name)

@@ -159,6 +159,7 @@ def test_combine_backward(T, K, E, D, gap, drop, dtype):
     ys[int(route.offsets[E]):] = float("nan")
     w = torch.rand((T, K), device=DEV) * 2 - 0.5
     w[route.place < 0] = float("nan")
+    gap += 3                                                    # (dys has a stride of its own)
     whole = torch.full((T * K, D + gap), 77.0, dtype=t, device=DEV)
     dys = whole[:, gap // 2:gap // 2 + D]
     dw = torch.full((T, K), float("nan"), device=DEV)
@@ -167,8 +168,7 @@ def test_combine_backward(T, K, E, D, gap, drop, dtype):
     assert (np.abs(f64(dys) - want_dys) <= (U + h) * np.abs(want_dys) * (1 + h) + TINY[t]).all()
     _, size = eo.expert_combine_backward(np.abs(f64(dy)), np.abs(f64(ys)), np.ones((T, K)), place, np.zeros((T * K, D)))
     assert (np.abs(f64(dw) - want_dw) <= (D / 64 + 16) * U * size).all()
-    if gap:
-        assert bool((whole[:, :gap // 2] == 77).all()) and bool((whole[:, gap // 2 + D:] == 77).all())
+    assert bool((whole[:, :gap // 2] == 77).all()) and bool((whole[:, gap // 2 + D:] == 77).all())
     # without weights and without the router's gradient: the rows' copies
     alone = torch.full((T * K, D), 77.0, dtype=t, device=DEV)
     kb.kfac_expert_combine_backward(route, dy, None, None, alone)
@@ -399,7 +399,8 @@ def test_bindings_refuse():
              lambda: kb.kfac_expert_dispatch(route, x.t().contiguous().t(), xs), lambda: kb.kfac_expert_dispatch(route, x.cpu(), xs.cpu()),
              lambda: kb.kfac_expert_combine(route, xs, w.double(), x), lambda: kb.kfac_expert_combine(route, xs, w[:5], x),
              lambda: kb.kfac_expert_combine(route, xs, w.cpu(), x), lambda: kb.kfac_expert_combine_backward(route, x, None, w, xs, w),
-             lambda: kb.kfac_expert_combine_backward(route, x, torch.zeros((12, 20), dtype=bf, device=DEV)[:, :16], w, xs, w.clone()),
+             lambda: kb.kfac_expert_combine_backward(route, x, torch.zeros((12, 20), dtype=bf, device=DEV), w, xs, w.clone()),
+             lambda: kb.kfac_expert_combine_backward(route, x, xs, w, torch.zeros((12, 16), device=DEV), w.clone()),
              lambda: kb.kfac_expert_factor(plan, xs.float(), route.offsets, out=F), lambda: kb.kfac_expert_factor(plan, xs[:11], route.offsets, out=F),
              lambda: kb.kfac_expert_factor(plan, xs, route.offsets.long(), out=F), lambda: kb.kfac_expert_factor(plan, xs, route.offsets[:3], out=F),
              lambda: kb.kfac_expert_factor(plan, xs, route.offsets), lambda: kb.kfac_expert_factor(plan, xs, route.offsets, out=F, running=F),

@@ -12,8 +12,8 @@ P = ctypes.c_void_p
 A, B, C, D = P(0x1000000), P(0x2000000), P(0x3000000), P(0x4000000)     # never dereferenced: every call below fails before a launch
 
 
-def desc(tokens=8, choices=2, experts=4, dim=64, dtype=kb.KFAC_BF16, ld_token=0, ld_row=0):
-    return kb.kfac_expert_desc(tokens, choices, experts, dim, dtype, ld_token, ld_row)
+def desc(tokens=8, choices=2, experts=4, dim=64, dtype=kb.KFAC_BF16, ld_token=0, ld_row=0, ld_grad=0):
+    return kb.kfac_expert_desc(tokens, choices, experts, dim, dtype, ld_token, ld_row, ld_grad)
 
 
 def fdesc(rows=64, experts=4, dim=64, dtype=kb.KFAC_BF16, has_bias=0, packed=0, ld=0):
@@ -22,13 +22,13 @@ def fdesc(rows=64, experts=4, dim=64, dtype=kb.KFAC_BF16, has_bias=0, packed=0, 
 
 def test_struct_sizes_match_header():
     assert ctypes.sizeof(kb.kfac_grad_item) == 8 + 8 + 8 + 8
-    assert ctypes.sizeof(kb.kfac_expert_desc) == 24 + 2 * 8
+    assert ctypes.sizeof(kb.kfac_expert_desc) == 24 + 3 * 8
     assert ctypes.sizeof(kb.kfac_expert_factor_desc) == 6 * 4 + 8
 
 
 BAD_ROUTES = [dict(tokens=-1), dict(choices=0), dict(choices=65), dict(experts=0), dict(experts=1025), dict(tokens=1 << 30, choices=2)]
 BAD_ROWS = BAD_ROUTES + [dict(dim=0), dict(dim=(1 << 20) + 1), dict(dtype=3), dict(ld_token=63), dict(ld_row=63), dict(ld_row=-1),
-                         dict(ld_token=(1 << 28) + 1)]
+                         dict(ld_token=(1 << 28) + 1), dict(ld_grad=63), dict(ld_grad=(1 << 28) + 1)]
 
 
 @pytest.mark.parametrize("change", BAD_ROUTES, ids=str)
