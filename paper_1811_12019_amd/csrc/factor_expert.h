@@ -3,8 +3,8 @@
 //
 // Cut.  Rows of an expert are cut into ranges of rows_per, which the host chooses from the rows of all experts; how many ranges there are is
 // known on the device only.  A launch has workgroups for the most there can be: rows / rows_per whole ones and a part for every expert, times
-// the tiles.  Every workgroup reads the offsets, adds up the ranges before each expert's (one scan of up to 1024 experts, well below a
-// microsecond against a tile's 10) and finds its own; those behind the last range end.  Ranges of all experts, tiles inside a range, are one work list
+// the tiles.  Every wavefront reads the offsets, adds up the ranges before each expert's (one scan in registers) and finds its own; those behind
+// the last range end.  Ranges of all experts, tiles inside a range, are one work list
 // that is dealt to the XCDs as any build's (unit_of): the tiles of a range, which read the same rows, share an L2.
 // An expert of one range goes straight to its destination; the others' partial sums are added up by a second launch, which there is if
 // an expert can have more than rows_per rows at all.
@@ -30,8 +30,6 @@ struct ExpertArgs {
     int ranges, parts;       // the most there can be
 };
 
-constexpr int EXPERT_LDS_INTS = 32;
-
 // What a workgroup works on.
 struct ExpertRange {
     int expert, sub, ranges; // range `sub` of `ranges` of the expert
@@ -40,81 +38,76 @@ struct ExpertRange {
 };
 
 // Rows of expert e: offsets that lie outside or descend are cut off.
-__device__ __forceinline__ void expert_rows(const ExpertArgs& a, int e, int& row, int& rows) {
-    const gint* o = as_global((int*)a.offsets);
-    const int r0 = min(max(o[e], 0), a.rows), r1 = min(max(o[e + 1], r0), a.rows);
+__device__ __forceinline__ void expert_rows(const ExpertArgs& a, int from, int to, int& row, int& rows) {
+    const int r0 = min(max(from, 0), a.rows), r1 = min(max(to, r0), a.rows);
     row = r0;
     rows = r1 - r0;
 }
 
+// Sums of the lanes up to and with this one: within rows of 16 lanes, then across them.
+__device__ __forceinline__ unsigned wave_scan(unsigned v) {
+#define KFAC_SCAN_STEP(ctrl, rows) v += (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, rows, 0xf, false)
+    KFAC_SCAN_STEP(0x111, 0xf);        // row_shr 1, 2, 4, 8
+    KFAC_SCAN_STEP(0x112, 0xf);
+    KFAC_SCAN_STEP(0x114, 0xf);
+    KFAC_SCAN_STEP(0x118, 0xf);
+    KFAC_SCAN_STEP(0x142, 0xa);        // row_bcast 15: rows 0 and 2 to 1 and 3
+    KFAC_SCAN_STEP(0x143, 0xc);        // row_bcast 31: rows 0 and 1 to 2 and 3
+#undef KFAC_SCAN_STEP
+    return v;
+}
+
 // Of the ranges of all experts (SPLIT: of the experts of several ranges) the one that `pick` names from their number (-1: none).  False: none.
+// Every wavefront works it out by itself, some experts to a lane: without LDS and barriers.
 template <bool SPLIT, class Pick>
-__device__ __forceinline__ bool expert_range(const ExpertArgs& a, int* lds, Pick&& pick, ExpertRange& out) {
-    const int t = threadIdx.x, nt = blockDim.x, lane = t & 63, wave = t >> 6, waves = nt >> 6;
-    const int per = (a.experts + nt - 1) / nt, e0 = t * per;
-    unsigned key = 0, part = 0;                                        // of this thread's experts
-    auto ranges_of = [&](int e, int& row, int& rows) -> int {
-        expert_rows(a, e, row, rows);
-        const int n = (int)(((unsigned)rows + a.rows_per - 1) / (unsigned)a.rows_per);
+__device__ __forceinline__ bool expert_range(const ExpertArgs& a, Pick&& pick, ExpertRange& out) {
+    const int lane = threadIdx.x & 63, per = (a.experts + 63) >> 6, e0 = lane * per, e1 = min(e0 + per, a.experts);
+    const gint* o = as_global((int*)a.offsets);
+    auto ranges_of = [&](int rows) -> unsigned {
+        const unsigned n = ((unsigned)rows + a.rows_per - 1) / (unsigned)a.rows_per;
         return n == 0 && a.mode != OUT_EMA ? 1 : n;                    // (an average without rows stays as it is)
     };
-    for (int e = e0; e < e0 + per && e < a.experts; ++e) {
-        int row, rows;
-        const unsigned n = ranges_of(e, row, rows);
+    unsigned key = 0, part = 0;                                        // of this lane's experts
+    int row = 0, rows = 0;                                             // of the last of them
+    unsigned n = 0;
+    auto take = [&](int from, int to) {
+        expert_rows(a, from, to, row, rows);
+        n = ranges_of(rows);
+    };
+    int at = o[min(e0, a.experts)];
+#pragma unroll 8
+    for (int e = e0; e < e1; ++e) {
+        const int next = o[e + 1];
+        take(at, next);
+        at = next;
         key += SPLIT ? (n > 1) : n;
         part += n > 1 ? n : 0;
     }
-    unsigned k = key, p = part;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const unsigned ku = __shfl_up(k, off, 64), pu = __shfl_up(p, off, 64);
-        if (lane >= off) {
-            k += ku;
-            p += pu;
-        }
-    }
-    if (lane == 63) {
-        lds[wave] = (int)k;
-        lds[8 + wave] = (int)p;
-    }
-    __syncthreads();
-    unsigned all = 0, kb = 0, pb = 0;
-    for (int w = 0; w < waves; ++w) {
-        if (w < wave) {
-            kb += (unsigned)lds[w];
-            pb += (unsigned)lds[8 + w];
-        }
-        all += (unsigned)lds[w];
-    }
+    unsigned k = wave_scan(key), p = wave_scan(part);
+    unsigned all = (unsigned)__builtin_amdgcn_readlane((int)k, 63);
     if (all > (unsigned)a.ranges) all = (unsigned)a.ranges;            // (offsets that do not ascend could name more)
-    const int want = pick((int)all);                                   // (the same in all threads)
+    const int want = pick((int)all);                                   // (the same in all lanes)
     if (want < 0 || (unsigned)want >= all) return false;
-    kb += k - key;
-    pb += p - part;
-    if ((unsigned)want >= kb && (unsigned)want < kb + key) {
-        for (int e = e0;; ++e) {                                       // (ends inside this thread's experts)
-            int row, rows;
-            const unsigned n = ranges_of(e, row, rows), mine = SPLIT ? (n > 1) : n;
-            if ((unsigned)want < kb + mine) {
-                lds[16] = e;
-                lds[17] = want - (int)kb;
-                lds[18] = (int)n;
-                lds[19] = (int)pb;
-                lds[20] = row;
-                lds[21] = rows;
-                break;
-            }
-            kb += mine;
-            pb += n > 1 ? n : 0;
-        }
+    auto owner_of = [&]() { return __builtin_amdgcn_readfirstlane(__ffsll(__ballot((unsigned)want >= k - key && (unsigned)want < k)) - 1); };
+    int owner = owner_of(), first = 0;
+    if (per > 1) {                                                     // the owner's experts, one to a lane
+        first = owner * per;
+        const unsigned kb = (unsigned)__builtin_amdgcn_readlane((int)(k - key), owner), pb = (unsigned)__builtin_amdgcn_readlane((int)(p - part), owner);
+        const int e = min(first + min(lane, per - 1), a.experts - 1);
+        take(o[e], o[e + 1]);
+        const bool own = lane < per && first + lane < a.experts;
+        key = own ? (SPLIT ? (n > 1) : n) : 0;
+        part = own && n > 1 ? n : 0;
+        k = kb + wave_scan(key);
+        p = pb + wave_scan(part);
+        owner = owner_of();
     }
-    __syncthreads();
-    out.expert = __builtin_amdgcn_readfirstlane(lds[16]);
-    out.sub = __builtin_amdgcn_readfirstlane(lds[17]);
-    out.ranges = __builtin_amdgcn_readfirstlane(lds[18]);
-    out.part = __builtin_amdgcn_readfirstlane(lds[19]);
-    out.row = __builtin_amdgcn_readfirstlane(lds[20]);
-    out.rows = __builtin_amdgcn_readfirstlane(lds[21]);
+    out.expert = first + owner;
+    out.sub = want - __builtin_amdgcn_readlane((int)(k - key), owner);
+    out.ranges = __builtin_amdgcn_readlane((int)n, owner);
+    out.part = __builtin_amdgcn_readlane((int)(p - part), owner);
+    out.row = __builtin_amdgcn_readlane(row, owner);
+    out.rows = __builtin_amdgcn_readlane(rows, owner);
     return out.ranges == 1 || (long long)out.part + out.ranges <= a.parts;
 }
 
@@ -171,7 +164,7 @@ void expert_tile_kernel(ExpertArgs a) {
     constexpr int ES = KIND == 2 ? 4 : 2;
     ExpertRange r;
     int tile = 0;
-    const bool there = expert_range<false>(a, (int*)(smem + tile_lds_bytes<TW, ES>()), [&](int all) {
+    const bool there = expert_range<false>(a, [&](int all) {
         const int unit = unit_of(all * a.ntiles, blockIdx.x, 0);
         const int range = unit < 0 ? -1 : unit / a.ntiles;
         tile = unit - range * a.ntiles;
@@ -208,7 +201,7 @@ void expert_tile_kernel(ExpertArgs a) {
 
 template <int TW, int KIND>
 static int launch_expert_tile_kernel(const char* name, const ExpertArgs& a, unsigned wgs, hipStream_t stream) {
-    constexpr int ES = KIND == 2 ? 4 : 2, LDS = tile_lds_bytes<TW, ES>() + EXPERT_LDS_INTS * 4;
+    constexpr int ES = KIND == 2 ? 4 : 2, LDS = tile_lds_bytes<TW, ES>();
     if constexpr (LDS > 64 * 1024) {                                   // (see launch_tile_kernel)
         if (hipFuncSetAttribute((const void*)expert_tile_kernel<TW, KIND>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess)
             return KFAC_ERR_HIP;

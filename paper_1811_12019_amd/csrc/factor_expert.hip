@@ -25,11 +25,10 @@ __global__ __launch_bounds__(256) void expert_pad_kernel(const char* x, const in
 template <int GROUPS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4, 8))) void expert_reduce_kernel(ExpertArgs a, int per) {
     __shared__ __attribute__((aligned(16))) float lds[GROUPS == 1 ? 32 * 33 : RD_MANY_FLOATS];
-    __shared__ int found[EXPERT_LDS_INTS];
     ExpertRange r;
     unsigned unit = 0, last = 0;
     int j = 0;
-    bool there = expert_range<true>(a, found, [&](int all) {
+    bool there = expert_range<true>(a, [&](int all) {
         const unsigned units = (unsigned)all * (unsigned)per, each = units / gridDim.x, more = units - each * gridDim.x;
         unit = blockIdx.x * each + min(blockIdx.x, more);
         last = unit + each + (blockIdx.x < more);
@@ -40,8 +39,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4, 8))) voi
         if (in == (unsigned)per) {
             in = 0;
             ++j;
-            __syncthreads();
-            there = expert_range<true>(a, found, [&](int) { return j; }, r);
+            there = expert_range<true>(a, [&](int) { return j; }, r);
         }
         if (there) {
             FactorPlan pl;
