@@ -28,6 +28,7 @@ struct ExpertArgs {
     float scale, decay;
     int rows_per, tw, tiles_dim, ntiles, tile_floats;
     int ranges, parts;       // the most there can be
+    int streams;             // results go past the caches
 };
 
 // What a workgroup works on.
@@ -157,7 +158,7 @@ __device__ __forceinline__ void expert_zeros(gfloat* out, size_t count, int shar
 }
 
 // (the tile kernel's launch bounds: factor_launch.h)
-template <int TW, int KIND>
+template <int TW, int KIND, bool STREAM>
 __global__ __launch_bounds__((tile_threads<TW, KIND == 2 ? 4 : 2>())) __attribute__((amdgpu_waves_per_eu(TW == 256 || KIND == 2 ? 2 : 3, 8)))
 void expert_tile_kernel(ExpertArgs a) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
@@ -191,24 +192,24 @@ void expert_tile_kernel(ExpertArgs a) {
     const KFAC_AS1 unsigned char* x = (const KFAC_AS1 unsigned char*)a.x + (size_t)(r.row + first) * a.ld * ES;
     const OutSpec os = expert_out(a, r.expert);
     if (job.I == job.J) {
-        if (TW == 128 && a.tw == 64) factor_tile_run<TW == 128 ? 64 : TW, KIND, FEED_PIXELS, true>(v, x, job, os, smem);
-        else factor_tile_run<TW, KIND, FEED_PIXELS, true>(v, x, job, os, smem);
+        if (TW == 128 && a.tw == 64) factor_tile_run<TW == 128 ? 64 : TW, KIND, FEED_PIXELS, true, STREAM>(v, x, job, os, smem);
+        else factor_tile_run<TW, KIND, FEED_PIXELS, true, STREAM>(v, x, job, os, smem);
     } else {
-        if (TW == 128 && a.tw == 64) factor_tile_run<TW == 128 ? 64 : TW, KIND, FEED_PIXELS, false>(v, x, job, os, smem);
-        else factor_tile_run<TW, KIND, FEED_PIXELS, false>(v, x, job, os, smem);
+        if (TW == 128 && a.tw == 64) factor_tile_run<TW == 128 ? 64 : TW, KIND, FEED_PIXELS, false, STREAM>(v, x, job, os, smem);
+        else factor_tile_run<TW, KIND, FEED_PIXELS, false, STREAM>(v, x, job, os, smem);
     }
 }
 
-template <int TW, int KIND>
+template <int TW, int KIND, bool STREAM>
 static int launch_expert_tile_kernel(const char* name, const ExpertArgs& a, unsigned wgs, hipStream_t stream) {
     constexpr int ES = KIND == 2 ? 4 : 2, LDS = tile_lds_bytes<TW, ES>();
     if constexpr (LDS > 64 * 1024) {                                   // (see launch_tile_kernel)
-        if (hipFuncSetAttribute((const void*)expert_tile_kernel<TW, KIND>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess)
+        if (hipFuncSetAttribute((const void*)expert_tile_kernel<TW, KIND, STREAM>, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess)
             return KFAC_ERR_HIP;
     }
     void* tok = nullptr;
     if (timing_enabled()) timing_begin(name, stream, &tok);
-    hipLaunchKernelGGL((expert_tile_kernel<TW, KIND>), dim3(wgs), dim3(tile_threads<TW, ES>()), LDS, stream, a);
+    hipLaunchKernelGGL((expert_tile_kernel<TW, KIND, STREAM>), dim3(wgs), dim3(tile_threads<TW, ES>()), LDS, stream, a);
     if (tok) timing_end(stream, tok);
     if (hipGetLastError() != hipSuccess) return KFAC_ERR_HIP;
     return KFAC_OK;
@@ -220,10 +221,11 @@ int launch_expert_tiles(const ExpertArgs& a, unsigned wgs, hipStream_t stream)
 #ifdef KFAC_EXPERT_KIND
 {
     if constexpr (KIND != 2) {
-        if (a.tw == 256) return launch_expert_tile_kernel<256, KIND>("expert_tile_kernel<256, 16-bit>", a, wgs, stream);
-        return launch_expert_tile_kernel<128, KIND>("expert_tile_kernel<128, 16-bit>", a, wgs, stream);
+        if (a.tw == 256 && a.streams) return launch_expert_tile_kernel<256, KIND, true>("expert_tile_kernel<256, 16-bit, stream>", a, wgs, stream);
+        if (a.tw == 256) return launch_expert_tile_kernel<256, KIND, false>("expert_tile_kernel<256, 16-bit>", a, wgs, stream);
     }
-    return launch_expert_tile_kernel<128, KIND>("expert_tile_kernel<128, f32>", a, wgs, stream);
+    if (a.streams) return launch_expert_tile_kernel<128, KIND, true>(KIND == 2 ? "expert_tile_kernel<128, f32, stream>" : "expert_tile_kernel<128, 16-bit, stream>", a, wgs, stream);
+    return launch_expert_tile_kernel<128, KIND, false>(KIND == 2 ? "expert_tile_kernel<128, f32>" : "expert_tile_kernel<128, 16-bit>", a, wgs, stream);
 }
 template int launch_expert_tiles<KFAC_EXPERT_KIND>(const ExpertArgs&, unsigned, hipStream_t);
 #else

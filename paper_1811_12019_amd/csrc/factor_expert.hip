@@ -88,6 +88,11 @@ static bool expert_factor_ok(const kfac_expert_factor_desc* d) {
 //     512 columns, 8 experts of 64 rows 8.3 and 10.4; of 256 10.3 and 12.4; 32 of 64 15.9 and 13.2; fp32, 256 columns, 8 of 256 16 and 21; 8 of 2,048 32 and 30
 // Rows of a range: 1,024 columns, 256 wide, 32 of 4,096 1,024 298, 2,048 246, 6,400 211; 8 of 4,096 86, 69, 111; 512 columns, 128 wide, 8 of 4,096
 // 1,024 36, 1,536 34, 3,072 46; fp32, 1,024 columns, 8 of 1,024 256 108, 512 100, 1,024 118; 512 columns, 64 of 1,024 512 195, 1,024 200, 1,600 213.
+// Results (in rows of whole cache lines: parts of lines written past the caches cost as much again, 1,233 columns 206 and 318 us) go past the caches
+// where they do not stay in the 256 MB memory-side one anyway beside what else a step touches.  bf16, us, kept and past them: 64 experts of 64 rows and
+// 512 columns (64 MB) 18.2 and 19.0, as running averages 22.2 and 27.9; 32 of 256 rows and 1,024 columns (128 MB) 49.7 and 38.6, 57 and 53; 32 of 512 rows
+// and 2,048 columns (512 MB) 187 and 153, 229 and 196.
+constexpr size_t EXPERT_STREAM = (size_t)96 << 20;
 constexpr double FEW_WGS = 160, WIDE_TILE_ROWS = 200000;
 
 static ExpertCut expert_cut(const kfac_expert_factor_desc& d) {
@@ -171,6 +176,7 @@ extern "C" int kfac_expert_factor(const kfac_expert_factor_desc* desc, const voi
     a.tile_floats = c.tile_floats;
     a.ranges = (int)c.ranges;
     a.parts = (int)c.parts;
+    a.streams = a.mode != OUT_PACKED && a.dout % 32 == 0 && (uintptr_t)dst % 128 == 0 && a.result * sizeof(float) * d.experts > EXPERT_STREAM;
     const long long wgs = (c.ranges * c.ntiles + 7) / 8 * 8;
     // (Four workgroups to a part, which share out its rows and its sums, where there are many ranges to an expert and few parts: 64 columns, 4 experts
     // of 16 ranges 15.0 -> 13.4 us, 192 columns, 2 of 10 16.5 -> 14.9; 256 columns, 8 of 8, 384 parts, 23.8 and 26.8.)

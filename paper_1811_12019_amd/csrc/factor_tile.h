@@ -347,8 +347,8 @@ constexpr int SPLIT_PRODUCTS = 8;
 constexpr int split_a(int e) { return e < 2 ? e + 1 : e < 5 ? e - 2 : e < 7 ? e - 5 : 0; }       // 1 2 0 1 2 0 1 0
 constexpr int split_b(int e) { return e < 2 ? 2 - e : e < 5 ? 4 - e : e < 7 ? 6 - e : 0; }       // 2 1 2 1 0 1 0 0
 
-// One tile.  KIND 0: bf16, 1: fp16, 2: fp32.
-template <int TW, int KIND, int FEED, bool DIAG>
+// One tile.  KIND 0: bf16, 1: fp16, 2: fp32.  STREAM: results of whole cache lines to a row, which go past the caches (factor_expert.h).
+template <int TW, int KIND, int FEED, bool DIAG, bool STREAM = false>
 __device__ __forceinline__ void factor_tile_run(const View& v, const KFAC_AS1 unsigned char* x, const TileJob& job,
                                                 const OutSpec& os, unsigned char* smem) {
     constexpr bool PLAIN = FEED == FEED_PIXELS, WINDOW = FEED == FEED_WINDOW, PLANES = FEED == FEED_PLANES;
@@ -792,6 +792,7 @@ __device__ __forceinline__ void factor_tile_run(const View& v, const KFAC_AS1 un
     // for every pass do not fit the registers beside the accumulators and the old values.)
     const unsigned out_bytes = packed ? 2u * d * (d + 1) : 4u * d * d;      // (d < 32768)
     const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)out, 0, out_bytes, 0x00027000);
+    constexpr int NT = STREAM ? 2 : 0;                             // (the buffer instructions' non-temporal bit)
     const unsigned ud = 4u * d;
     const unsigned direct0 = (I * TW + wr + vr) * ud + 4u * (J * TW + wc + vc);
     const unsigned mirror0 = (J * TW + wc + (lane >> 3)) * ud + 4u * (I * TW + wr + (lane & 7) * 4);
@@ -802,7 +803,7 @@ __device__ __forceinline__ void factor_tile_run(const View& v, const KFAC_AS1 un
         const OldAt at = old_at(ema & whole(p), direct0, ud);
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const v4u x = __builtin_amdgcn_raw_buffer_load_b128(rsrc, at.offset, pass_row(W, p, k) * at.row, 0);
+            const v4u x = __builtin_amdgcn_raw_buffer_load_b128(rsrc, at.offset, pass_row(W, p, k) * at.row, NT);
             __builtin_memcpy(&o[k], &x, 16);
         }
     };
@@ -811,7 +812,7 @@ __device__ __forceinline__ void factor_tile_run(const View& v, const KFAC_AS1 un
     auto put_vector = [&](unsigned off, unsigned step, const v4f& val) {
         v4u x;
         __builtin_memcpy(&x, &val, 16);
-        __builtin_amdgcn_raw_buffer_store_b128(x, rsrc, off + step, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(x, rsrc, off + step, 0, NT);
     };
     // Elsewhere: element by element.  Elements that are not there (beyond the matrix, padding, the other half of a diagonal
     // tile) get an offset outside the buffer, which the hardware drops: no branches, so that many are in flight.  (One body for the mirror

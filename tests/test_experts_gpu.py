@@ -343,6 +343,34 @@ def test_factor_of_many_rows(rows, E, dim, dtype):
             check_factor(f64(S[e:e + 1]), f64(new)[None], ema=True)
 
 
+@pytest.mark.parametrize("dtype,dim", [("bf16", 512), ("f32", 448), ("bf16", 192)])
+def test_factor_results_past_the_caches(dtype, dim):
+    """Results of more than 96 MB, in rows of whole cache lines (another kernel, its name says so), against fewer experts' (the same bits)."""
+    E, per = (100 << 20) // (4 * dim * dim), 50
+    x = rows_of(E * per, dim, TYPES[dtype], 0, dim)
+    offsets = torch.arange(0, E * per + 1, per, dtype=torch.int32, device=DEV)
+    S = torch.randn((E, dim, dim), device=DEV)
+    S = S + S.transpose(1, 2)
+    want = S.clone()
+    out = torch.empty_like(S)
+    plan = kb.ExpertFactors(E * per, E, dim, TYPES[dtype])
+    kb.kfac_kernel_timing_enable(True)
+    try:
+        kb.kfac_expert_factor(plan, x, offsets, out=out)
+        kb.kfac_expert_factor(plan, x, offsets, running=S, decay=0.9)
+        assert any("stream>" in k for k in kb.kfac_kernel_timing_report())
+    finally:
+        kb.kfac_kernel_timing_enable(False)
+    some = 3
+    few = kb.ExpertFactors(some * per, some, dim, TYPES[dtype])
+    part = torch.empty((some, dim, dim), device=DEV)
+    for e in (0, E // 2, E - some):
+        kb.kfac_expert_factor(few, x[e * per:(e + some) * per], offsets[:some + 1], out=part)
+        assert torch.equal(out[e:e + some], part)
+        kb.kfac_expert_factor(few, x[e * per:(e + some) * per], offsets[:some + 1], running=want[e:e + some], decay=0.9)
+        assert torch.equal(S[e:e + some], want[e:e + some])
+
+
 def test_factor_of_rows_beyond_32_bits():
     """Rows 2^17 elements apart: the last of 36,000 begins 9.4 GB in."""
     rows, E, dim, ld = 36000, 3, 48, 1 << 17
