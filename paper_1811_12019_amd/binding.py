@@ -469,11 +469,15 @@ def _gpu(device, where: str) -> torch.device:
 
 def _stream_on(index: int, where: str, stream) -> int:
     """The stream of a call on tensors of GPU `index`, which has to be the current one."""
-    get = getattr(torch._C, "_cuda_getDevice", None)
-    current = torch.cuda.current_device() if get is None else get()
+    private = torch._C              # (see _stream; there is a tensor, so that the GPU is initialised)
+    try:
+        current = private._cuda_getDevice()
+        found = private._cuda_getCurrentRawStream(current) if stream is None else None
+    except AttributeError:
+        current, found = torch.cuda.current_device(), None
     if current != index:
         _want(False, where, f"the tensors' device {index} is not the current one, {current}")
-    return _stream(stream)
+    return _stream(stream) if found is None else found
 
 
 def _flat(t: torch.Tensor, dtype: torch.dtype, shape, device, where: str, name: str) -> torch.Tensor:
@@ -505,12 +509,15 @@ class GradBatch:
         self.count = n
         self.keep = (list(g), out)
         self.host = (kfac_grad_item * max(n, 1))()
+        index = self.device.index
         for i, (x, y) in enumerate(zip(g, out)):
-            _want(x.dtype in _KFAC_DTYPE and x.device == self.device and (x.numel() == 0 or _dense(x)), "GradBatch",
-                  f"gradient {i}: float32, bfloat16 or float16 on {self.device}, without gaps")
-            _want(y is None or (y.dtype == x.dtype and y.device == x.device and y.shape == x.shape and y.stride() == x.stride()), "GradBatch",
-                  f"result {i}: the gradient's type, shape and strides")
-            self.host[i] = kfac_grad_item(x.data_ptr(), _ptr(y), x.numel(), _KFAC_DTYPE[x.dtype])
+            dtype, size = _KFAC_DTYPE.get(x.dtype), x.numel()
+            if dtype is None or x.get_device() != index or not (x.is_contiguous() or _dense(x)):
+                _want(size == 0 and dtype is not None, "GradBatch", f"gradient {i}: float32, bfloat16 or float16 on {self.device}, without gaps")
+            if y is not None and not (y.dtype == x.dtype and y.get_device() == index and y.shape == x.shape and y.stride() == x.stride()):
+                _want(False, "GradBatch", f"result {i}: the gradient's type, shape and strides")
+            item = self.host[i]
+            item.g, item.out, item.n, item.dtype = x.data_ptr(), None if y is None else y.data_ptr(), size, dtype
         self.norm = torch.zeros((), dtype=torch.float32, device=self.device)
         self.ws = alloc_workspace(int(load_library().kfac_grad_norm_workspace_bytes(self.host, n)), self.device)
         self.ws_bytes = 0 if self.ws is None else self.ws.numel()
@@ -518,8 +525,8 @@ class GradBatch:
 
 def kfac_grad_norm_batched(batch: GradBatch, stream=None) -> torch.Tensor:
     """The norm over all of the table's gradients: batch.norm, a device float that the next call on the table overwrites."""
-    rc = load_library().kfac_grad_norm_batched(batch.host, batch.count, batch.norm.data_ptr(), _ptr(batch.ws), batch.ws_bytes,
-                                               _stream_on(batch.device.index, "kfac_grad_norm_batched", stream))
+    rc = (_lib or load_library()).kfac_grad_norm_batched(batch.host, batch.count, batch.norm.data_ptr(), _ptr(batch.ws), batch.ws_bytes,
+                                                         _stream_on(batch.device.index, "kfac_grad_norm_batched", stream))
     _check(rc, "kfac_grad_norm_batched")
     return batch.norm
 
@@ -531,9 +538,9 @@ def kfac_grad_clip_batched(batch: GradBatch, max_norm: float, given_norm: Option
     if given_norm is not None and not (given_norm.dtype == torch.float32 and given_norm.numel() == 1 and given_norm.device == batch.device):
         _want(False, where, f"given_norm: one float32 on {batch.device}")
     norm = batch.norm if given_norm is None else given_norm
-    rc = load_library().kfac_grad_clip_batched(batch.host, batch.count, float(max_norm), _ptr(given_norm),
-                                               None if given_norm is not None else norm.data_ptr(), _ptr(batch.ws), batch.ws_bytes,
-                                               _stream_on(batch.device.index, where, stream))
+    rc = (_lib or load_library()).kfac_grad_clip_batched(batch.host, batch.count, float(max_norm), _ptr(given_norm),
+                                                         None if given_norm is not None else norm.data_ptr(), _ptr(batch.ws), batch.ws_bytes,
+                                                         _stream_on(batch.device.index, where, stream))
     _check(rc, where)
     return norm
 
@@ -598,9 +605,9 @@ def kfac_expert_sort(route: ExpertRoute, expert: torch.Tensor, stream=None) -> E
     """expert: (T, K) int32, what is not in 0 .. E - 1 is no assignment.  Fills route.offsets, route.order and route.place."""
     if not (expert.dtype == torch.int32 and expert.shape == route.place.shape and expert.is_contiguous() and expert.get_device() == route.index):
         _want(False, "kfac_expert_sort", f"expert: contiguous int32 of shape {tuple(route.place.shape)} on {route.device}")
-    rc = load_library().kfac_expert_sort(ctypes.byref(route.desc), expert.data_ptr(), route.offsets.data_ptr(), _ptr(route.order),
-                                         route.place.data_ptr(), _ptr(route.ws), route.ws_bytes,
-                                         _stream_on(route.index, "kfac_expert_sort", stream))
+    rc = (_lib or load_library()).kfac_expert_sort(ctypes.byref(route.desc), expert.data_ptr(), route.offsets.data_ptr(), _ptr(route.order),
+                                                   route.place.data_ptr(), _ptr(route.ws), route.ws_bytes,
+                                                   _stream_on(route.index, "kfac_expert_sort", stream))
     _check(rc, "kfac_expert_sort")
     return route
 
@@ -608,8 +615,8 @@ def kfac_expert_sort(route: ExpertRoute, expert: torch.Tensor, stream=None) -> E
 def kfac_expert_dispatch(route: ExpertRoute, x: torch.Tensor, xs: torch.Tensor, stream=None) -> torch.Tensor:
     """x: (T, D), xs: (T K, D): every token's row to its places."""
     desc = route._rows("kfac_expert_dispatch", x, xs)
-    rc = load_library().kfac_expert_dispatch(desc, x.data_ptr(), route.place.data_ptr(), xs.data_ptr(),
-                                             _stream_on(route.index, "kfac_expert_dispatch", stream))
+    rc = (_lib or load_library()).kfac_expert_dispatch(desc, x.data_ptr(), route.place.data_ptr(), xs.data_ptr(),
+                                                       _stream_on(route.index, "kfac_expert_dispatch", stream))
     _check(rc, "kfac_expert_dispatch")
     return xs
 
@@ -617,8 +624,8 @@ def kfac_expert_dispatch(route: ExpertRoute, x: torch.Tensor, xs: torch.Tensor, 
 def kfac_expert_combine(route: ExpertRoute, ys: torch.Tensor, weights: Optional[torch.Tensor], y: torch.Tensor, stream=None) -> torch.Tensor:
     """ys: (T K, D), weights: (T, K) float32 or None (all 1), y: (T, D).  Without weights also the gradient of kfac_expert_dispatch."""
     desc = route._rows("kfac_expert_combine", y, ys)
-    rc = load_library().kfac_expert_combine(desc, ys.data_ptr(), route._weights(weights, "kfac_expert_combine", "weights"),
-                                            route.place.data_ptr(), y.data_ptr(), _stream_on(route.index, "kfac_expert_combine", stream))
+    rc = (_lib or load_library()).kfac_expert_combine(desc, ys.data_ptr(), route._weights(weights, "kfac_expert_combine", "weights"),
+                                                      route.place.data_ptr(), y.data_ptr(), _stream_on(route.index, "kfac_expert_combine", stream))
     _check(rc, "kfac_expert_combine")
     return y
 
@@ -629,9 +636,9 @@ def kfac_expert_combine_backward(route: ExpertRoute, dy: torch.Tensor, ys: Optio
     where = "kfac_expert_combine_backward"
     _want(dweights is None or ys is not None, where, "dweights needs ys")
     desc = route._rows(where, dy, None if dweights is None else ys, dys)
-    rc = load_library().kfac_expert_combine_backward(desc, dy.data_ptr(), None if dweights is None else ys.data_ptr(),
-                                                     route._weights(weights, where, "weights"), route.place.data_ptr(), dys.data_ptr(),
-                                                     route._weights(dweights, where, "dweights"), _stream_on(route.index, where, stream))
+    rc = (_lib or load_library()).kfac_expert_combine_backward(desc, dy.data_ptr(), None if dweights is None else ys.data_ptr(),
+                                                               route._weights(weights, where, "weights"), route.place.data_ptr(), dys.data_ptr(),
+                                                               route._weights(dweights, where, "dweights"), _stream_on(route.index, where, stream))
     _check(rc, where)
     return dys
 
@@ -667,8 +674,8 @@ def kfac_expert_factor(plan: ExpertFactors, x: torch.Tensor, offsets: torch.Tens
     to = running if out is None else out
     if not (to.dtype == torch.float32 and to.shape == plan.shape and to.is_contiguous() and to.get_device() == plan.index):
         _want(False, where, f"contiguous float32 results of shape {plan.shape} on {plan.device}")
-    rc = load_library().kfac_expert_factor(ctypes.byref(plan.desc), x.data_ptr(), offsets.data_ptr(), float(scale), _ptr(out), _ptr(running),
-                                           float(decay), _ptr(plan.ws), plan.ws_bytes, _stream_on(plan.index, where, stream))
+    rc = (_lib or load_library()).kfac_expert_factor(ctypes.byref(plan.desc), x.data_ptr(), offsets.data_ptr(), float(scale), _ptr(out), _ptr(running),
+                                                     float(decay), _ptr(plan.ws), plan.ws_bytes, _stream_on(plan.index, where, stream))
     _check(rc, where)
     return to
 
