@@ -21,11 +21,15 @@ constexpr int EX_MAX_EXPERTS = 1024, EX_MAX_CHOICES = 64, EX_MAX_DIM = 1 << 20;
 struct SortCut {
     int blocks, waves, per_wave;          // assignments of a wavefront, a multiple of 64
     int bits;                             // of an expert's number
+    int group;                            // runs that a workgroup of the first kernel counts
     int width;                            // threads of the second kernel that read a run's counts, 8 each: a power of two
     int lds;                              // bytes of the second kernel
 };
 constexpr int SORT_STEPS = 2, SORT_STEPS_MANY = 8, SORT_BLOCKS = 256, SORT_ALONE = 6144;
-constexpr long long SORT_RUN_MAX = 32768;  // counts have 16 bits
+// Runs that one workgroup counts: of many experts several, since every workgroup of the second kernel reads all counts (524,288 assignments to
+// 64, 256, 512 and 1,000 experts with 1 11.8, 14.1, 17.9 and 29.6 us, with 4 12.4, 13.6, 15.4 and 17.4).
+constexpr int SORT_GROUP = 4, SORT_GROUP_EXPERTS = 256;
+constexpr long long SORT_RUN_MAX = 16128;  // (counts of SORT_GROUP runs have 16 bits)
 
 static SortCut sort_cut(int n, int experts) {
     SortCut c;
@@ -43,6 +47,7 @@ static SortCut sort_cut(int n, int experts) {
     c.per_wave = std::max((int)((per + 63) / 64 * 64), 64);
     const long long run = (long long)c.per_wave * c.waves;
     c.blocks = (int)std::max((n + run - 1) / run, 1ll);
+    c.group = experts >= SORT_GROUP_EXPERTS ? SORT_GROUP : 1;
     c.bits = 0;
     while ((1 << c.bits) < experts) ++c.bits;
     c.width = 1;
@@ -51,26 +56,59 @@ static SortCut sort_cut(int n, int experts) {
     return c;
 }
 
-// A run's experts, counted: counts[blockIdx][e], 8 * width of them.
-__global__ __launch_bounds__(1024) void expert_count_kernel(const int* expert, int n, int experts, int per_block, int width, uint16_t* counts) {
-    __shared__ int cnt[EX_MAX_EXPERTS];
+static unsigned count_wgs(const SortCut& c) { return (unsigned)((c.blocks + c.group - 1) / c.group); }
+
+// The experts of `group` runs, counted: of all of them, counts[blockIdx][e], and of those before each, ahead[run][e], 8 * width of either.
+__global__ __launch_bounds__(1024) void expert_count_kernel(const int* expert, int n, int experts, int per_block, int blocks, int group, int width, uint16_t* counts,
+                                                            uint16_t* ahead) {
+    __shared__ int cnt[SORT_GROUP][EX_MAX_EXPERTS];
     const int t = threadIdx.x, nt = blockDim.x;
-    for (int e = t; e < 8 * width; e += nt) cnt[e] = 0;
+    for (int k = 0; k < group; ++k)
+        for (int e = t; e < 8 * width; e += nt) cnt[k][e] = 0;
     __syncthreads();
-    const long long i0 = (long long)blockIdx.x * per_block, i1 = i0 + per_block < n ? i0 + per_block : n;
+    const int run0 = blockIdx.x * group, steps = per_block / nt;      // (a run is whole steps of the workgroup)
+    const long long i0 = (long long)run0 * per_block + t;
+    auto count = [&](int k, int e) {
+        if ((unsigned)e < (unsigned)experts) atomicAdd(&cnt[k][e], 1);
+    };
+    if (group == 1) {
+        const long long i1 = min((long long)(run0 + 1) * per_block, (long long)n);
 #pragma unroll 4
-    for (long long i = i0 + t; i < i1; i += nt) {
-        const int e = expert[i];
-        if ((unsigned)e < (unsigned)experts) atomicAdd(&cnt[e], 1);
+        for (long long i = i0; i < i1; i += nt) count(0, expert[i]);
+    } else {
+        for (int j0 = 0; j0 < group * steps; j0 += 8) {
+            int e[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const long long i = i0 + (long long)(j0 + j) * nt;
+                e[j] = j0 + j < group * steps && i < n ? expert[i] : -1;
+            }
+            int k = j0 / steps, left = (k + 1) * steps - j0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                count(k, e[j]);
+                if (--left == 0) {
+                    ++k;
+                    left = steps;
+                }
+            }
+        }
     }
     __syncthreads();
-    for (int e = t; e < 8 * width; e += nt) counts[(size_t)blockIdx.x * (8 * width) + e] = (uint16_t)cnt[e];
+    for (int e = t; e < 8 * width; e += nt) {
+        int sum = 0;
+        for (int k = 0; k < group; ++k) {
+            if (run0 + k < blocks) ahead[(size_t)(run0 + k) * (8 * width) + e] = (uint16_t)sum;
+            sum += cnt[k][e];
+        }
+        counts[(size_t)blockIdx.x * (8 * width) + e] = (uint16_t)sum;
+    }
 }
 
 // STEPS: a wavefront's assignments and their ranks stay in registers (0: are looked up again).
 template <int STEPS>
-__global__ __launch_bounds__(1024) void expert_place_kernel(const int* expert, int n, int experts, int per_wave, int bits, int width,
-                                                            const uint16_t* counts, int* offsets, int* order, int* place) {
+__global__ __launch_bounds__(1024) void expert_place_kernel(const int* expert, int n, int experts, int per_wave, int bits, int group, int width,
+                                                            const uint16_t* counts, const uint16_t* ahead, int* offsets, int* order, int* place) {
     extern __shared__ int lds[];
     const int t = threadIdx.x, nt = blockDim.x, lane = t & 63, wave = t >> 6, waves = nt >> 6;
     int* cnt = lds;                                     // [waves][experts]: a wavefront's counts, then where its rows go
@@ -87,20 +125,25 @@ __global__ __launch_bounds__(1024) void expert_place_kernel(const int* expert, i
         for (int k = 0; k < STEPS; ++k) held[k] = i0 + 64 * k + lane < i1 ? expert[i0 + 64 * k + lane] : -1;
     }
     for (int e = t; e < waves * experts + 16 * width; e += nt) cnt[e] = 0;
-    // The counts of all runs and of those before this one: groups of `width` threads share out the runs, a thread takes 8 experts.
+    // The counts of all runs and of those before this one: groups of `width` threads share out what there is of them, a thread takes 8 experts.
     int all[8] = {}, some[8] = {};
-    const int col = t & (width - 1), groups = nt / width;
-    if (nblk > 1) {
-#pragma unroll 4
-        for (int b = t / width; b < nblk; b += groups) {
-            const u4 c = *(const KFAC_AS1 u4*)((const gchar*)counts + ((size_t)b * width + col) * 16);
+    const int col = t & (width - 1), lists = (nblk + group - 1) / group;
+    // (four rows of counts to a thread: the fewer threads, the fewer sums to add up; 65,536 assignments to 8 experts 10.1 -> 8.6 us)
+    const int adders = nblk > 1 ? min(nt, max(64, ((lists + 3) / 4 * width + 63) / 64 * 64)) : 0, groups = adders / width;
+    if (t < adders) {                                   // (whole wavefronts)
+        const int mine = blk / group;
+        auto eight = [&](const uint16_t* from, int row, bool to_all, bool to_some) {
+            const u4 c = *(const KFAC_AS1 u4*)((const gchar*)from + ((size_t)row * width + col) * 16);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const int v = (int)(c[k / 2] >> (k & 1) * 16 & 0xffff);
-                all[k] += v;
-                some[k] += b < blk ? v : 0;
+                all[k] += to_all ? v : 0;
+                some[k] += to_some ? v : 0;
             }
-        }
+        };
+        if (group > 1 && t < width) eight(ahead, blk, false, true);
+#pragma unroll 8
+        for (int b = t / width; b < lists; b += groups) eight(counts, b, true, b < mine);
         for (int off = width; off < 64; off <<= 1) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
@@ -110,7 +153,7 @@ __global__ __launch_bounds__(1024) void expert_place_kernel(const int* expert, i
         }
     }
     __syncthreads();
-    if (nblk > 1 && lane < width) {
+    if (t < adders && lane < width) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             if (all[k]) atomicAdd(&total[k * width + col], all[k]);
@@ -417,7 +460,7 @@ static size_t moved(const RowArgs& a, int token_rows, int sorted_rows) { return 
 extern "C" size_t kfac_expert_sort_workspace_bytes(const kfac_expert_desc* desc) {
     if (!route_ok(desc)) return 0;
     const SortCut c = sort_cut(desc->tokens * desc->choices, desc->experts);
-    return c.blocks > 1 ? align_up((size_t)c.blocks * c.width * 16, 256) : 0;
+    return c.blocks > 1 ? align_up((size_t)(c.blocks + count_wgs(c)) * c.width * 16, 256) : 0;
 }
 
 extern "C" int kfac_expert_sort(const kfac_expert_desc* desc, const int32_t* expert, int32_t* offsets, int32_t* order, int32_t* place,
@@ -436,14 +479,16 @@ extern "C" int kfac_expert_sort(const kfac_expert_desc* desc, const int32_t* exp
     const SortCut c = sort_cut(n, E);
     hipStream_t st = (hipStream_t)stream;
     const int threads = 64 * c.waves;
-    if (c.blocks > 1) KFAC_LAUNCH(expert_count_kernel, dim3(c.blocks), dim3(threads), st, expert, n, E, c.waves * c.per_wave,
-                                  c.width, (uint16_t*)ws);
+    uint16_t* counts = (uint16_t*)ws;
+    uint16_t* ahead = c.blocks > 1 ? counts + (size_t)count_wgs(c) * c.width * 8 : nullptr;
+    if (c.blocks > 1)
+        KFAC_LAUNCH(expert_count_kernel, dim3(count_wgs(c)), dim3(threads), st, expert, n, E, c.waves * c.per_wave, c.blocks, c.group, c.width, counts, ahead);
     void* tok = nullptr;
     if (timing_enabled()) timing_begin("expert_place_kernel", st, &tok);
     auto kernel = c.per_wave <= 64 * SORT_STEPS        ? expert_place_kernel<SORT_STEPS>
                   : c.per_wave <= 64 * SORT_STEPS_MANY ? expert_place_kernel<SORT_STEPS_MANY>
                                                        : expert_place_kernel<0>;
-    hipLaunchKernelGGL(kernel, dim3(c.blocks), dim3(threads), c.lds, st, expert, n, E, c.per_wave, c.bits, c.width, (const uint16_t*)ws, offsets,
+    hipLaunchKernelGGL(kernel, dim3(c.blocks), dim3(threads), c.lds, st, expert, n, E, c.per_wave, c.bits, c.group, c.width, counts, ahead, offsets,
                        n > 0 ? order : nullptr, place);
     if (tok) timing_end(st, tok);
     KFAC_LAUNCH_CHECK();
