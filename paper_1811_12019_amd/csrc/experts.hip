@@ -283,7 +283,10 @@ __device__ __forceinline__ void by_vector(int dim, unsigned c, F&& f) {
 }
 
 constexpr int GROUP = 4;                  // choices whose rows are fetched together
-constexpr unsigned BACK_WORKGROUP = 256;  // vectors of a row from which on a whole workgroup takes a token
+// Vectors of a row from which on a whole workgroup takes a token's gradients, and tokens up to which it does so for rows of more than 64: the
+// rows of a token are then on their way at once.  bf16, us, a wavefront and a workgroup to a token: 16,384 tokens x 4 of 2,048 values (256 vectors) 113 and 103,
+// 8,192 x 2 of 1,024 (128) 15.1 and 19.4, 8,192 x 4 of 1,700 78 and 84; 16 x 8 of 4,096 13.3 and 7.5.  Short rows take part of a wavefront.
+constexpr unsigned BACK_WORKGROUP = 256;
 constexpr int BACK_FEW = 512;
 
 template <int ES, bool STREAM>
@@ -340,16 +343,17 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(RowArgs a, const ch
     });
 }
 
-// WAVES wavefronts per token; dy's row is fetched once for every GROUP choices.
-template <int KIND, bool STREAM, int WAVES>
+// LANES threads per token: part of a wavefront, one, or a workgroup; dy's row is fetched once for every GROUP choices.
+template <int KIND, bool STREAM, int LANES>
 __global__ __launch_bounds__(256) void expert_combine_backward_kernel(RowArgs a, int tokens, const char* dy, const char* ys, const float* weights,
                                                                       const int* place, char* dys, float* dweights) {
-    constexpr int ES = elem_bytes<KIND>, V = elems16<KIND>;
+    constexpr int ES = elem_bytes<KIND>, V = elems16<KIND>, ACROSS = LANES < 64 ? LANES : 64;
     __shared__ float red[GROUP][4];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const unsigned token = WAVES == 4 ? blockIdx.x : blockIdx.x * 4u + wave;
-    if (token >= (unsigned)tokens) return;                             // (WAVES = 4: never)
-    const size_t at = (size_t)token * a.choices;
+    const int lane = threadIdx.x & (LANES - 1);
+    unsigned token = blockIdx.x * (256u / LANES) + threadIdx.x / LANES;
+    if constexpr (LANES >= 64) token = __builtin_amdgcn_readfirstlane(token);
+    const bool in = token < (unsigned)tokens;                          // (a workgroup for a token: always)
+    const size_t at = (size_t)(in ? token : 0) * a.choices;
     for (int k0 = 0; k0 < a.choices; k0 += GROUP) {
         int row[GROUP];
         float w[GROUP], dot[GROUP];
@@ -357,11 +361,12 @@ __global__ __launch_bounds__(256) void expert_combine_backward_kernel(RowArgs a,
         for (int k = 0; k < GROUP; ++k) {
             const int i = min(k0 + k, a.choices - 1);
             const int r = place[at + i];
-            row[k] = __builtin_amdgcn_readfirstlane(k0 + k < a.choices && (unsigned)r < (unsigned)a.rows ? r : -1);
+            row[k] = in && k0 + k < a.choices && (unsigned)r < (unsigned)a.rows ? r : -1;
+            if constexpr (LANES >= 64) row[k] = __builtin_amdgcn_readfirstlane(row[k]);
             w[k] = weights ? weights[at + i] : 1.f;
             dot[k] = 0.f;
         }
-        for (unsigned c = WAVES == 4 ? threadIdx.x : lane; c < a.per_row; c += 64 * WAVES) {
+        for (unsigned c = lane; in && c < a.per_row; c += LANES) {
             by_vector<ES>(a.dim, c, [&](auto whole, long long in_row, int some, int shared) {
                 const int count = decltype(whole)::value ? V : some;
                 const u4 d = load_row16<ES>((const gchar*)dy + token * a.ld_token + in_row, count);
@@ -382,7 +387,7 @@ __global__ __launch_bounds__(256) void expert_combine_backward_kernel(RowArgs a,
                 }
 #pragma unroll
                 for (int k = 0; k < GROUP; ++k) {
-                    if (row[k] < 0) continue;                          // (uniform)
+                    if (row[k] < 0) continue;
 #pragma unroll
                     for (int j = 0; j < V; ++j) f[j] = g[j] * w[k];
                     store_row16<ES, STREAM>((gchar*)dys + row[k] * a.ld_grad + in_row, pack16<KIND>(f), count);
@@ -393,14 +398,14 @@ __global__ __launch_bounds__(256) void expert_combine_backward_kernel(RowArgs a,
 #pragma unroll
             for (int k = 0; k < GROUP; ++k) {
 #pragma unroll
-                for (int off = 32; off > 0; off >>= 1) dot[k] += __shfl_down(dot[k], off, 64);
-                if (WAVES == 1 && lane == 0 && k0 + k < a.choices) dweights[at + k0 + k] = row[k] >= 0 ? dot[k] : 0.f;
-                if (WAVES == 4 && lane == 0) red[k][wave] = row[k] >= 0 ? dot[k] : 0.f;
+                for (int off = ACROSS / 2; off > 0; off >>= 1) dot[k] += __shfl_down(dot[k], off, ACROSS);
+                const float sum = row[k] >= 0 ? dot[k] : 0.f;
+                if (LANES <= 64 && lane == 0 && in && k0 + k < a.choices) dweights[at + k0 + k] = sum;
+                if (LANES == 256 && (lane & 63) == 0) red[k][lane >> 6] = sum;
             }
-            if constexpr (WAVES == 4) {
-                const int k = threadIdx.x;
+            if constexpr (LANES == 256) {
                 __syncthreads();
-                if (k < GROUP && k0 + k < a.choices) dweights[at + k0 + k] = (red[k][0] + red[k][1]) + (red[k][2] + red[k][3]);
+                if (lane < GROUP && k0 + lane < a.choices) dweights[at + k0 + lane] = (red[lane][0] + red[lane][1]) + (red[lane][2] + red[lane][3]);
                 __syncthreads();
             }
         }
@@ -545,12 +550,13 @@ extern "C" int kfac_expert_combine_backward(const kfac_expert_desc* desc, const 
         constexpr int KIND = decltype(kind)::value;
         constexpr bool STREAM = decltype(streams)::value;
         const char* name = STREAM ? "expert_combine_backward_kernel<stream>" : "expert_combine_backward_kernel";
-        if (a.per_row >= BACK_WORKGROUP || (desc->tokens <= BACK_FEW && a.per_row > 64))
-            KFAC_LAUNCH_AS(name, (expert_combine_backward_kernel<KIND, STREAM, 4>), dim3(desc->tokens), dim3(256), (hipStream_t)stream, a, desc->tokens,
-                           (const char*)dy, (const char*)ys, weights, place, (char*)dys, dweights);
-        else
-            KFAC_LAUNCH_AS(name, (expert_combine_backward_kernel<KIND, STREAM, 1>), dim3((desc->tokens + 3) / 4), dim3(256), (hipStream_t)stream, a,
-                           desc->tokens, (const char*)dy, (const char*)ys, weights, place, (char*)dys, dweights);
-        return KFAC_OK;
+        auto launch = [&](auto lanes) -> int {
+            constexpr int LANES = decltype(lanes)::value;
+            KFAC_LAUNCH_AS(name, (expert_combine_backward_kernel<KIND, STREAM, LANES>), dim3((unsigned)((desc->tokens + 256ll / LANES - 1) / (256 / LANES))),
+                           dim3(256), (hipStream_t)stream, a, desc->tokens, (const char*)dy, (const char*)ys, weights, place, (char*)dys, dweights);
+            return KFAC_OK;
+        };
+        if (a.per_row >= BACK_WORKGROUP || (desc->tokens <= BACK_FEW && a.per_row > 64)) return launch(IntConstant<256>{});
+        return a.per_row > 32 ? launch(IntConstant<64>{}) : a.per_row > 8 ? launch(IntConstant<32>{}) : launch(IntConstant<8>{});
     });
 }
