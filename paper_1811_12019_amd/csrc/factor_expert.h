@@ -4,8 +4,10 @@
 // Cut.  Rows of an expert are cut into ranges of rows_per, which the host chooses from the rows of all experts; how many ranges there are is
 // known on the device only.  A launch has workgroups for the most there can be: rows / rows_per whole ones and a part for every expert, times
 // the tiles.  Every wavefront reads the offsets, adds up the ranges before each expert's (one scan in registers) and finds its own; those behind
-// the last range end.  Ranges of all experts, tiles inside a range, are one work list
-// that is dealt to the XCDs as any build's (unit_of): the tiles of a range, which read the same rows, share an L2.
+// the last range end.  Ranges of all experts, tiles inside a range, are one work list, of which every XCD gets a contiguous part, so that the tiles of a
+// range, which read the same rows, share an L2 (tiles of 2, 4 and 8 ranges in turns: 387 -> 502, 634 and 534 us): an eighth of the units, or, where they take
+// several rounds, of the work (equal numbers of experts of unequal rows left XCDs waiting: 65,536 rows of 2,048 columns, 32 experts of softmax(0.5 z) and
+// softmax(2 z) of them, 375 -> 341 and 574 -> 409 us; of equal experts 330 and 337).
 // An expert of one range goes straight to its destination; the others' partial sums are added up by a second launch, which there is if
 // an expert can have more than rows_per rows at all.
 // Addresses.  A workgroup takes its range's first row for the tensor's beginning and its last one for the end: offsets inside it fit 32 bits
@@ -29,6 +31,7 @@ struct ExpertArgs {
     int rows_per, tw, tiles_dim, ntiles, tile_floats;
     int ranges, parts;       // the most there can be
     int streams;             // results go past the caches
+    float beside;            // what a tile costs beside its rows, in rows (0: units are dealt by number, not by work)
 };
 
 // What a workgroup works on.
@@ -45,9 +48,10 @@ __device__ __forceinline__ void expert_rows(const ExpertArgs& a, int from, int t
     rows = r1 - r0;
 }
 
-// Sums of the lanes up to and with this one: within rows of 16 lanes, then across them.
-__device__ __forceinline__ unsigned wave_scan(unsigned v) {
-#define KFAC_SCAN_STEP(ctrl, rows) v += (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, rows, 0xf, false)
+// Sums of the lanes up to and with this one (unsigned or float): within rows of 16 lanes, then across them.
+template <class T>
+__device__ __forceinline__ T wave_scan(T v) {
+#define KFAC_SCAN_STEP(ctrl, rows) v += __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), ctrl, rows, 0xf, false))
     KFAC_SCAN_STEP(0x111, 0xf);        // row_shr 1, 2, 4, 8
     KFAC_SCAN_STEP(0x112, 0xf);
     KFAC_SCAN_STEP(0x114, 0xf);
@@ -58,8 +62,9 @@ __device__ __forceinline__ unsigned wave_scan(unsigned v) {
     return v;
 }
 
-// Of the ranges of all experts (SPLIT: of the experts of several ranges) the one that `pick` names from their number (-1: none).  False: none.
-// Every wavefront works it out by itself, some experts to a lane: without LDS and barriers.
+// Of the ranges of all experts (SPLIT: of the experts of several ranges) the one that `pick` names (-1: none).  False: none.
+// Every wavefront works it out by itself, some experts to a lane: without LDS and barriers.  pick(all, units_before): the number of ranges, and a function that
+// tells how many of their tiles lie before a fraction of all the work (experts' rows and `beside` for each range; a lane's experts count as alike).
 template <bool SPLIT, class Pick>
 __device__ __forceinline__ bool expert_range(const ExpertArgs& a, Pick&& pick, ExpertRange& out) {
     const int lane = threadIdx.x & 63, per = (a.experts + 63) >> 6, e0 = lane * per, e1 = min(e0 + per, a.experts);
@@ -71,6 +76,7 @@ __device__ __forceinline__ bool expert_range(const ExpertArgs& a, Pick&& pick, E
     unsigned key = 0, part = 0;                                        // of this lane's experts
     int row = 0, rows = 0;                                             // of the last of them
     unsigned n = 0;
+    int there_rows = 0;
     auto take = [&](int from, int to) {
         expert_rows(a, from, to, row, rows);
         n = ranges_of(rows);
@@ -83,11 +89,23 @@ __device__ __forceinline__ bool expert_range(const ExpertArgs& a, Pick&& pick, E
         at = next;
         key += SPLIT ? (n > 1) : n;
         part += n > 1 ? n : 0;
+        there_rows += rows;
     }
     unsigned k = wave_scan(key), p = wave_scan(part);
     unsigned all = (unsigned)__builtin_amdgcn_readlane((int)k, 63);
     if (all > (unsigned)a.ranges) all = (unsigned)a.ranges;            // (offsets that do not ascend could name more)
-    const int want = pick((int)all);                                   // (the same in all lanes)
+    // (With `beside` at least an average range's rows, an eighth of the work is at most a quarter of the units.)
+    auto units_before = [&](float fraction) -> unsigned {
+        const float some = wave_scan((float)there_rows), total = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, some), 63));
+        const float beside = max(a.beside, total / (float)max(all, 1u)), work = (float)there_rows + beside * (float)key;
+        const float upto = some + beside * (float)k, goal = (total + beside * (float)all) * fraction;
+        const unsigned long long beyond = __ballot(upto > goal);
+        if (!beyond || fraction >= 1.f) return all * a.ntiles;
+        const float inside = work > 0.f ? max(goal - (upto - work), 0.f) / work : 0.f;
+        const unsigned tiles = key * a.ntiles, mine = (k - key) * a.ntiles + min((unsigned)(inside * (float)tiles), tiles);
+        return min((unsigned)__builtin_amdgcn_readlane((int)mine, __builtin_amdgcn_readfirstlane(__ffsll(beyond) - 1)), all * a.ntiles);
+    };
+    const int want = pick((int)all, units_before);                     // (the same in all lanes)
     if (want < 0 || (unsigned)want >= all) return false;
     auto owner_of = [&]() { return __builtin_amdgcn_readfirstlane(__ffsll(__ballot((unsigned)want >= k - key && (unsigned)want < k)) - 1); };
     int owner = owner_of(), first = 0;
@@ -165,9 +183,17 @@ void expert_tile_kernel(ExpertArgs a) {
     constexpr int ES = KIND == 2 ? 4 : 2;
     ExpertRange r;
     int tile = 0;
-    const bool there = expert_range<false>(a, [&](int all) {
-        const int unit = unit_of(all * a.ntiles, blockIdx.x, 0);
-        const int range = unit < 0 ? -1 : unit / a.ntiles;
+    const bool there = expert_range<false>(a, [&](int all, auto&& units_before) {
+        int unit;
+        if (a.beside > 0.f) {                                          // workgroups k, k + 8, ..: the eighth of the work that XCD k gets
+            const int xcd = blockIdx.x & 7;
+            unit = (int)((xcd ? units_before(0.125f * xcd) : 0) + (blockIdx.x >> 3));
+            if (unit >= (int)units_before(0.125f * (xcd + 1))) return -1;
+        } else {
+            unit = unit_of(all * a.ntiles, blockIdx.x, 0);
+            if (unit < 0) return -1;
+        }
+        const int range = unit / a.ntiles;
         tile = unit - range * a.ntiles;
         return range;
     }, r);

@@ -28,7 +28,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4, 8))) voi
     ExpertRange r;
     unsigned unit = 0, last = 0;
     int j = 0;
-    bool there = expert_range<true>(a, [&](int all) {
+    bool there = expert_range<true>(a, [&](int all, auto&&) {
         const unsigned units = (unsigned)all * (unsigned)per, each = units / gridDim.x, more = units - each * gridDim.x;
         unit = blockIdx.x * each + min(blockIdx.x, more);
         last = unit + each + (blockIdx.x < more);
@@ -39,7 +39,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4, 8))) voi
         if (in == (unsigned)per) {
             in = 0;
             ++j;
-            there = expert_range<true>(a, [&](int) { return j; }, r);
+            there = expert_range<true>(a, [&](int, auto&&) { return j; }, r);
         }
         if (there) {
             FactorPlan pl;
@@ -177,7 +177,13 @@ extern "C" int kfac_expert_factor(const kfac_expert_factor_desc* desc, const voi
     a.ranges = (int)c.ranges;
     a.parts = (int)c.parts;
     a.streams = a.mode != OUT_PACKED && a.dout % 32 == 0 && (uintptr_t)dst % 128 == 0 && a.result * sizeof(float) * d.experts > EXPERT_STREAM;
-    const long long wgs = (c.ranges * c.ntiles + 7) / 8 * 8;
+    // Where the tiles take several rounds, an XCD gets an eighth of their work and not of their number; it may then have twice as many (see
+    // units_before; and some, for what the fractions are rounded to), and workgroups that find nothing left end.
+    const long long most = c.ranges * c.ntiles;
+    const float beside = c.tw == 256 ? 1000.f : f32 ? 200.f : 400.f;
+    const bool by_work = most > 2 * (c.tw == 256 ? 256 : f32 ? 512 : 768) && d.rows >= 0.5f * beside * c.ranges;   // (of few rows units are alike)
+    a.beside = by_work ? beside : 0.f;
+    const long long wgs = by_work ? (most / 4 + 16) * 8 : (most + 7) / 8 * 8;
     // (Four workgroups to a part, which share out its rows and its sums, where there are many ranges to an expert and few parts: 64 columns, 4 experts
     // of 16 ranges 15.0 -> 13.4 us, 192 columns, 2 of 10 16.5 -> 14.9; 256 columns, 8 of 8, 384 parts, 23.8 and 26.8.)
     const int groups = d.rows / d.experts >= 4 * c.rows_per && (long long)d.experts * c.ntiles * (c.tw / 32) * (c.tw / 32) <= 256 ? 4 : 1;
