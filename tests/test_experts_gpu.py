@@ -343,6 +343,34 @@ def test_factor_of_many_rows(rows, E, dim, dtype):
             check_factor(f64(S[e:e + 1]), f64(new)[None], ema=True)
 
 
+@pytest.mark.parametrize("rows,E,dim,dtype", [(60000, 60, 768, "bf16"), (60000, 90, 640, "f16"), (30000, 90, 384, "f32"), (60000, 700, 200, "bf16")])
+def test_factor_tiles_dealt_by_work(rows, E, dim, dtype):
+    """More tiles than the chip takes in two rounds, of experts of few, of many and of all the rows, one and several experts to a lane of the
+    search: every expert against the reference on the GPU in 64 bits."""
+    x = rows_of(rows, dim, TYPES[dtype], 0, dim).relu()
+    rng = np.random.default_rng(dim)
+    share = np.exp(2 * rng.standard_normal(E))
+    skewed = np.concatenate([[0], np.minimum(np.round(np.cumsum(share / share.sum()) * rows), rows)]).astype(np.int64)
+    for cut in (bounds(rows, E, "even", 0), bounds(rows, E, "uneven", dim), bounds(rows, E, "one", 0), skewed):
+        offsets = torch.tensor(cut, dtype=torch.int32, device=DEV)
+        plan = kb.ExpertFactors(rows, E, dim, TYPES[dtype])
+        out = torch.full(plan.shape, float("nan"), device=DEV)
+        kb.kfac_expert_factor(plan, x, offsets, out=out)
+        S = torch.eye(dim, device=DEV).repeat(E, 1, 1)
+        kb.kfac_expert_factor(plan, x, offsets, running=S, decay=0.5)
+        for e in range(E):
+            n = int(cut[e + 1] - cut[e])
+            if n == 0:
+                assert not bool(out[e].any()) and torch.equal(S[e], torch.eye(dim, device=DEV))
+                continue
+            a = x[int(cut[e]):int(cut[e + 1])].double()
+            want = torch.mm(a.t().contiguous(), a) / n
+            off = out[e].double() - want
+            assert float(off.norm()) <= FACTOR_TOL * float(want.norm()) and float(off.abs().max()) <= FACTOR_TOL * float(want.abs().max()), e
+            new = 0.5 * torch.eye(dim, device=DEV).double() + 0.5 * want
+            assert float((S[e].double() - new).abs().max()) <= (FACTOR_TOL + 2e-7) * float(new.abs().max()), e
+
+
 @pytest.mark.parametrize("dtype,dim", [("bf16", 512), ("f32", 448), ("bf16", 192)])
 def test_factor_results_past_the_caches(dtype, dim):
     """Results of more than 96 MB, in rows of whole cache lines (another kernel, its name says so), against fewer experts' (the same bits)."""
