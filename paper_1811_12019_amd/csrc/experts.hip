@@ -29,7 +29,7 @@ constexpr int SORT_STEPS = 2, SORT_STEPS_MANY = 8, SORT_BLOCKS = 256, SORT_ALONE
 // Runs that one workgroup counts: of many experts several, since every workgroup of the second kernel reads all counts (524,288 assignments to
 // 64, 256, 512 and 1,000 experts with 1 11.8, 14.1, 17.9 and 29.6 us, with 4 12.4, 13.6, 15.4 and 17.4).
 constexpr int SORT_GROUP = 4, SORT_GROUP_EXPERTS = 256;
-constexpr long long SORT_RUN_MAX = 16128;  // (counts of SORT_GROUP runs have 16 bits)
+constexpr long long SORT_RUN_MAX = 15360;  // (counts of SORT_GROUP runs have 16 bits; whole steps of 8 and of 16 wavefronts)
 
 static SortCut sort_cut(int n, int experts) {
     SortCut c;

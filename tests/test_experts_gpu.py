@@ -80,6 +80,19 @@ def test_sort(T, K, E, how):
             np.testing.assert_array_equal(got.cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("E,n", [(256, 4200000), (700, 4128769), (256, 13000001), (100, 5000000)])
+def test_sort_of_long_runs_to_one_expert(E, n):
+    """All assignments of several runs in a row are one expert's: the most that a count of them has to hold."""
+    i = torch.arange(n, device=DEV, dtype=torch.int64)
+    expert = torch.where(i < n - 1000, E - 2, (i % E)).to(torch.int32)
+    order, by = torch.sort(expert.long(), stable=True)
+    want = torch.empty_like(by).scatter_(0, by, i)
+    route = kb.ExpertRoute(n, 1, E)
+    kb.kfac_expert_sort(route, expert.view(n, 1))
+    torch.testing.assert_close(route.offsets.long(), torch.cat([i[:1], torch.bincount(expert.long(), minlength=E).cumsum(0)]), rtol=0, atol=0)
+    assert torch.equal(route.place.view(-1).long(), want) and torch.equal(route.order.view(-1).long(), by)
+
+
 def test_sort_of_no_tokens_and_without_order():
     route = kb.ExpertRoute(0, 2, 5)
     route.offsets.fill_(7)
