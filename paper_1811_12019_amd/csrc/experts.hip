@@ -552,8 +552,10 @@ extern "C" int kfac_expert_combine_backward(const kfac_expert_desc* desc, const 
         const char* name = STREAM ? "expert_combine_backward_kernel<stream>" : "expert_combine_backward_kernel";
         auto launch = [&](auto lanes) -> int {
             constexpr int LANES = decltype(lanes)::value;
-            KFAC_LAUNCH_AS(name, (expert_combine_backward_kernel<KIND, STREAM, LANES>), dim3((unsigned)((desc->tokens + 256ll / LANES - 1) / (256 / LANES))),
-                           dim3(256), (hipStream_t)stream, a, desc->tokens, (const char*)dy, (const char*)ys, weights, place, (char*)dys, dweights);
+            const long long wgs = (desc->tokens + 256ll / LANES - 1) / (256 / LANES);
+            if (wgs * 256 > 0xffffffffll) return KFAC_ERR_TOO_LARGE;                            // (threads of a launch)
+            KFAC_LAUNCH_AS(name, (expert_combine_backward_kernel<KIND, STREAM, LANES>), dim3((unsigned)wgs), dim3(256),
+                           (hipStream_t)stream, a, desc->tokens, (const char*)dy, (const char*)ys, weights, place, (char*)dys, dweights);
             return KFAC_OK;
         };
         if (a.per_row >= BACK_WORKGROUP || (desc->tokens <= BACK_FEW && a.per_row > 64)) return launch(IntConstant<256>{});

@@ -89,6 +89,9 @@ def test_rows_refuse_pointers():
     assert lib.kfac_expert_combine_backward(d, A, B, None, C, B, D, None) == INVALID       # ys and dys
     many = ctypes.byref(desc(tokens=1 << 20, choices=1, dim=1 << 20))
     assert lib.kfac_expert_dispatch(many, A, B, C, None) == TOO_LARGE
+    for tokens, dim in [(1 << 29, 8), (200000000, 80)]:                                   # more threads than a launch has, of short rows
+        far = [P(k << 44) for k in range(1, 5)]
+        assert lib.kfac_expert_combine_backward(ctypes.byref(desc(tokens=tokens, choices=1, dim=dim)), far[0], far[1], None, far[2], far[3], None, None) == TOO_LARGE
 
 
 def test_nothing_to_do_launches_nothing():
