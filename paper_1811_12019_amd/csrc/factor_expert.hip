@@ -79,15 +79,18 @@ static bool expert_factor_ok(const kfac_expert_factor_desc* d) {
 // Width of the tiles and rows of a range, from the call's rows and experts of equal size.  Rows: as many as let all ranges run in as few rounds of the
 // workgroups that fit the chip (768, of 256-wide tiles 256, fp32 512 and one round more) as uncut experts would, counting half a range for every expert's
 // end, and not so few that a second range costs a tile more in partial sums than it saves; ranges near an average expert's rows are made longer, so that
-// most experts are one (three times as long where there are workgroups enough to even out the long ones); calls of few rows need no second launch.
-// Width: 64 where wider tiles would leave CUs without one, 256 from so many tile rows on that a workgroup outlasts its epilogue, with little padding.
+// most experts are one (three times as long where there are workgroups enough to even out the long ones); calls of few rows need no second launch
+// (fp32, us, with one and with two: 18 experts' 1,187 rows of 59 columns 11.3 and 14.9, 9 experts' 1,045 of 114 13.3 and 15.4, 5 experts' 1,240 of 32 13.2 and 11.7).
+// Width: 64 where wider tiles would leave CUs without one or cover much more than the matrix, 256 from so many tile rows on that a workgroup
+// outlasts its epilogue, with little padding.
 // Both sides, bf16, us (128- and 256-wide at the rows of a range that suit each best; 64- and 128-wide):
 //     512 columns, 8 experts of 4,096 rows 34 and 40; 32 of 1,024 39 and 46; 32 of 4,096 95 and 77; 128 of 1,024 98 and 94
 //     1,024 columns, 8 of 1,024 36 and 45; 8 of 4,096 78 and 69; 32 of 256 52 and 53; 32 of 1,024 105 and 93; 128 of 64 113 and 119; of 256 156 and 141
 //     2,048 columns, 8 of 256 40 and 48; 8 of 1,024 90 and 86; 32 of 64 115 and 118; 32 of 256 168 and 147; 32 of 1,024 345 and 257
+//     fp32, 30 of 1,000 rows, 192 columns 31 and 39, 256 43 and 41, 320 58 and 64; 80 of 132 rows, 329 columns 48 and 44
 //     512 columns, 8 experts of 64 rows 8.3 and 10.4; of 256 10.3 and 12.4; 32 of 64 15.9 and 13.2; fp32, 256 columns, 8 of 256 16 and 21; 8 of 2,048 32 and 30
 // Rows of a range: 1,024 columns, 256 wide, 32 of 4,096 1,024 298, 2,048 246, 6,400 211; 8 of 4,096 86, 69, 111; 512 columns, 128 wide, 8 of 4,096
-// 1,024 36, 1,536 34, 3,072 46; fp32, 1,024 columns, 8 of 1,024 256 108, 512 100, 1,024 118; 512 columns, 64 of 1,024 512 195, 1,024 200, 1,600 213.
+// 1,024 36, 1,536 34; fp32, 1,024 columns, 8 of 1,024 256 108, 512 100, 1,024 118; 512 columns, 64 of 1,024 512 195, 1,024 200, 1,600 213.
 // Results (in rows of whole cache lines: parts of lines written past the caches cost as much again, 1,233 columns 206 and 318 us) go past the caches
 // where they do not stay in the 256 MB memory-side one anyway beside what else a step touches.  bf16, us, kept and past them: 64 experts of 64 rows and
 // 512 columns (64 MB) 18.2 and 19.0, as running averages 22.2 and 27.9; 32 of 256 rows and 1,024 columns (128 MB) 49.7 and 38.6, 57 and 53; 32 of 512 rows
@@ -107,13 +110,14 @@ static ExpertCut expert_cut(const kfac_expert_factor_desc& d) {
     auto tiles = [&](int tw) { const double n = ceil_div(d.dim, tw); return 0.5 * n * (n + 1); };
     auto rows_of_width = [&](int tw) {
         const double slots = tw == 256 ? 256 : f32 ? 512 : 768, whole = tiles(tw) * d.experts, rounds = std::max(std::ceil(whole / slots), 1.0) + f32;
-        double r = std::max(rows * tiles(tw) / (0.95 * rounds * slots - 0.5 * whole), !f32 ? 1024.0 : tw == 64 ? 128.0 : 256.0);
+        double r = std::max(rows * tiles(tw) / (0.95 * rounds * slots - 0.5 * whole), !f32 ? 1024.0 : tw == 64 ? 128.0 : whole < slots ? 256.0 : 512.0);
         if (!f32 && r > 0.6 * each) r = std::max(r, (whole >= 2 * slots ? 3 : 1.5) * each);
-        if (rows <= (f32 ? 1024 : 2048) && (tw == 64 || !f32)) r = std::max(r, rows);
+        if (rows <= (f32 ? ROWS_PER_WG_MAX_F32 : 2048) && (tw == 64 || !f32)) r = std::max(r, rows);
         return (int)(std::min(r, (double)(f32 ? ROWS_PER_WG_MAX_F32 : ROWS_PER_WG_MAX)) + 63) / 64 * 64;
     };
     c.tw = 128;
-    if (d.dim <= 64 || tiles(128) * d.experts * std::max(1.0, std::ceil(each / rows_of_width(128))) < FEW_WGS) c.tw = 64;
+    const double fit = 0.25 * tiles(64) / tiles(128);
+    if (d.dim <= 64 || fit <= (f32 ? 0.7 : 0.55) || tiles(128) * d.experts * std::max(1.0, std::ceil(each / rows_of_width(128))) < FEW_WGS) c.tw = 64;
     else if (!f32 && d.dim > 128 && 4 * tiles(256) <= WIDE_PADDING * tiles(128) && tiles(256) * rows >= WIDE_TILE_ROWS) c.tw = 256;
     c.rows_per = rows_of_width(c.tw);
     c.tiles_dim = ceil_div(d.dim, c.tw);
