@@ -499,7 +499,8 @@ def _dense(t: torch.Tensor) -> bool:
 class GradBatch:
     """A kfac_grad_item table (host memory; built once, reused every step), its scratch and the device float `norm`.
     g: gradient tensors of any of the three types, their elements side by side; out: None (clipped in place), or per tensor None / a
-    tensor of the same type, shape and strides that receives the clipped gradient.  Calls that use one table must not overlap in time."""
+    tensor of the same type, shape and strides that receives the clipped gradient.  A tensor that is written must not be there twice.
+    Calls that use one table must not overlap in time."""
 
     def __init__(self, g: Sequence[torch.Tensor], out: Optional[Sequence[Optional[torch.Tensor]]] = None, device="cuda"):
         n = len(g)
@@ -518,9 +519,24 @@ class GradBatch:
                 _want(False, "GradBatch", f"result {i}: the gradient's type, shape and strides")
             item = self.host[i]
             item.g, item.out, item.n, item.dtype = x.data_ptr(), None if y is None else y.data_ptr(), size, dtype
+        self.apart = None         # whether a clipping call may write: no tensor that it writes overlaps another (found by the first one)
         self.norm = torch.zeros((), dtype=torch.float32, device=self.device)
         self.ws = alloc_workspace(int(load_library().kfac_grad_norm_workspace_bytes(self.host, n)), self.device)
         self.ws_bytes = 0 if self.ws is None else self.ws.numel()
+
+    def _apart(self) -> bool:
+        spans = []                # first byte, behind the last one, written
+        for item, (g, _) in zip(self.host, zip(*self.keep)):
+            size, here = item.n * g.element_size(), item.out in (None, item.g)
+            if size:
+                spans += [(item.g, item.g + size, here)] + ([] if here else [(item.out, item.out + size, True)])
+        any_end = written_end = 0
+        for first, end, written in sorted(spans):
+            if first < (any_end if written else written_end):
+                return False
+            any_end = max(any_end, end)
+            written_end = max(written_end, end) if written else written_end
+        return True
 
 
 def kfac_grad_norm_batched(batch: GradBatch, stream=None) -> torch.Tensor:
@@ -537,6 +553,10 @@ def kfac_grad_clip_batched(batch: GradBatch, max_norm: float, given_norm: Option
     where = "kfac_grad_clip_batched"
     if given_norm is not None and not (given_norm.dtype == torch.float32 and given_norm.numel() == 1 and given_norm.device == batch.device):
         _want(False, where, f"given_norm: one float32 on {batch.device}")
+    if batch.apart is None:
+        batch.apart = batch._apart()
+    if not batch.apart:
+        _want(False, where, "a tensor that is written overlaps another of the table")
     norm = batch.norm if given_norm is None else given_norm
     rc = (_lib or load_library()).kfac_grad_clip_batched(batch.host, batch.count, float(max_norm), _ptr(given_norm),
                                                          None if given_norm is not None else norm.data_ptr(), _ptr(batch.ws), batch.ws_bytes,

@@ -143,6 +143,20 @@ def test_captured_and_replayed():
         assert torch.equal(one.norm, two.norm) and all(torch.equal(x, y) for x, y in zip(out_a, out_b))
 
 
+def test_tensors_that_are_written_are_apart():
+    a, b, c = (torch.ones(100, device=DEV) for _ in range(3))
+    refused = [([a, a], None), ([a, a[50:]], None), ([a, b], [b, None]), ([a, b], [c, c]),
+               ([a[:40], a[60:], a[39:41]], None)]
+    for g, out in refused:
+        with pytest.raises(kb.KfacError):
+            kb.kfac_grad_clip_batched(kb.GradBatch(g, out), 0.5)
+    twice = kb.GradBatch([a, a])
+    assert abs(float(kb.kfac_grad_norm_batched(twice)) - 200 ** 0.5) <= 200 ** 0.5 * U      # (one that is only read may be there twice)
+    assert bool((a == 1).all() and (b == 1).all())
+    for g, out in [([a, a], [b, c]), ([a[:50], a[50:]], None), ([b, c], [b, None]), ([a, a[:0]], None)]:
+        kb.kfac_grad_clip_batched(kb.GradBatch(g, out), 0.5)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 def test_deterministic(dtype):
     tensors = grads([100003, 50000, 999], [dtype], 5)
