@@ -288,6 +288,7 @@ constexpr int GROUP = 4;                  // choices whose rows are fetched toge
 // 8,192 x 2 of 1,024 (128) 15.1 and 19.4, 8,192 x 4 of 1,700 78 and 84; 16 x 8 of 4,096 13.3 and 7.5.  Short rows take part of a wavefront.
 constexpr unsigned BACK_WORKGROUP = 256;
 constexpr int BACK_FEW = 512;
+constexpr int DISPATCH_LONG = 4000;       // bytes
 
 template <int ES, bool STREAM>
 __global__ __launch_bounds__(256) void expert_dispatch_kernel(RowArgs a, const char* x, const int* place, char* xs) {
@@ -510,7 +511,10 @@ extern "C" int kfac_expert_dispatch(const kfac_expert_desc* desc, const void* x,
     const int es = desc->dtype == KFAC_F32 ? 4 : 2;
     if (!on_grid(x, es) || !on_grid(xs, es) || !on_grid(place, 4)) return KFAC_ERR_INVALID_ARG;
     if (rows_overlap(x, desc->tokens, a.ld_token, xs, a.rows, a.ld_row, (long long)a.dim * es)) return KFAC_ERR_INVALID_ARG;
-    return by_type(desc->dtype, moved(a, 1, 1), [&](auto kind, auto streams) -> int {
+    // Short rows that begin and end inside a half cache line are kept: past the caches each end costs a line (bf16, us, kept and past them: 126,030 tokens x 4
+    // of 260 columns 91 and 101; 16,384 x 4 of 2,001 76 and 77, of 2,008 74 and 73, of 2,048 66 and 51).
+    const bool halves = ((uintptr_t)xs | (uintptr_t)a.ld_row | (uintptr_t)a.dim * es) % 64 == 0;
+    return by_type(desc->dtype, halves || a.dim * es >= DISPATCH_LONG ? moved(a, 1, 1) : 0, [&](auto kind, auto streams) -> int {
         constexpr int ES = elem_bytes<decltype(kind)::value>;
         constexpr bool STREAM = decltype(streams)::value;
         KFAC_LAUNCH_AS(STREAM ? "expert_dispatch_kernel<stream>" : "expert_dispatch_kernel", (expert_dispatch_kernel<ES, STREAM>),

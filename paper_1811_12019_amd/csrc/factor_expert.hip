@@ -91,11 +91,11 @@ static bool expert_factor_ok(const kfac_expert_factor_desc* d) {
 //     512 columns, 8 experts of 64 rows 8.3 and 10.4; of 256 10.3 and 12.4; 32 of 64 15.9 and 13.2; fp32, 256 columns, 8 of 256 16 and 21; 8 of 2,048 32 and 30
 // Rows of a range: 1,024 columns, 256 wide, 32 of 4,096 1,024 298, 2,048 246, 6,400 211; 8 of 4,096 86, 69, 111; 512 columns, 128 wide, 8 of 4,096
 // 1,024 36, 1,536 34; fp32, 1,024 columns, 8 of 1,024 256 108, 512 100, 1,024 118; 512 columns, 64 of 1,024 512 195, 1,024 200, 1,600 213.
-// Results (in rows of whole cache lines: parts of lines written past the caches cost as much again, 1,233 columns 206 and 318 us) go past the caches
-// where they do not stay in the 256 MB memory-side one anyway beside what else a step touches.  bf16, us, kept and past them: 64 experts of 64 rows and
-// 512 columns (64 MB) 18.2 and 19.0, as running averages 22.2 and 27.9; 32 of 256 rows and 1,024 columns (128 MB) 49.7 and 38.6, 57 and 53; 32 of 512 rows
-// and 2,048 columns (512 MB) 187 and 153, 229 and 196.
-constexpr size_t EXPERT_STREAM = (size_t)96 << 20;
+// Results in rows of whole halves of cache lines go past the caches where two of them do not stay in the 256 MB memory-side one (smaller parts of lines
+// written past them cost as much again: 8,192 rows of 64 experts, 1,000 columns 96 and 119, 1,025 109 and 154; 88 experts' 1,233 206 and 318).  bf16, us, kept and
+// past them: 8,192 rows, 64 experts of 1,024 columns (256 MB) 64 and 56, of 1,008 90 and 63, as running averages 118 and 91; 32 of 1,008 (124 MB) 57 and 39,
+// 67 and 57; 56 of 736 (116 MB) 26.7 and 29.7, 34.6 and 42.5; 16 of 2,000 columns, 16,384 rows 168 and 118, 179 and 148; fp32, 64 of 816 78 and 56, 82 and 76.
+constexpr size_t EXPERT_STREAM = (size_t)120 << 20;
 constexpr double FEW_WGS = 160, WIDE_TILE_ROWS = 200000;
 
 static ExpertCut expert_cut(const kfac_expert_factor_desc& d) {
@@ -180,7 +180,7 @@ extern "C" int kfac_expert_factor(const kfac_expert_factor_desc* desc, const voi
     a.tile_floats = c.tile_floats;
     a.ranges = (int)c.ranges;
     a.parts = (int)c.parts;
-    a.streams = a.mode != OUT_PACKED && a.dout % 32 == 0 && (uintptr_t)dst % 128 == 0 && a.result * sizeof(float) * d.experts > EXPERT_STREAM;
+    a.streams = a.mode != OUT_PACKED && a.dout % 16 == 0 && (uintptr_t)dst % 64 == 0 && a.result * sizeof(float) * d.experts > EXPERT_STREAM;
     // Where the tiles take several rounds, an XCD gets an eighth of their work and not of their number; it may then have twice as many (see
     // units_before; and some, for what the fractions are rounded to), and workgroups that find nothing left end.
     const long long most = c.ranges * c.ntiles;

@@ -384,10 +384,10 @@ def test_factor_tiles_dealt_by_work(rows, E, dim, dtype):
             assert float((S[e].double() - new).abs().max()) <= (FACTOR_TOL + 2e-7) * float(new.abs().max()), e
 
 
-@pytest.mark.parametrize("dtype,dim", [("bf16", 512), ("f32", 448), ("bf16", 192)])
+@pytest.mark.parametrize("dtype,dim", [("bf16", 512), ("f32", 448), ("bf16", 192), ("f16", 208), ("bf16", 720)])
 def test_factor_results_past_the_caches(dtype, dim):
-    """Results of more than 96 MB, in rows of whole cache lines (another kernel, its name says so), against fewer experts' (the same bits)."""
-    E, per = (100 << 20) // (4 * dim * dim), 50
+    """Results of more than 120 MB, in rows of whole halves of cache lines (another kernel, its name says so), against fewer experts' (the same bits)."""
+    E, per = (130 << 20) // (4 * dim * dim), 50
     x = rows_of(E * per, dim, TYPES[dtype], 0, dim)
     offsets = torch.arange(0, E * per + 1, per, dtype=torch.int32, device=DEV)
     S = torch.randn((E, dim, dim), device=DEV)
