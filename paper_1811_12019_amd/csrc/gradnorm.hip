@@ -27,7 +27,13 @@ struct GradBatch {
 // Chunks c0 .. c1 - 1, tensor by tensor from tensor m on, which is the first one's or an earlier one: f(tensor, first element, behind the last one).
 template <int MAX, class F>
 __device__ __forceinline__ void for_chunks(const GradBatch<MAX>& b, unsigned c0, unsigned c1, int& m, F&& f) {
-    while (b.prefix[m + 1] <= c0) ++m;
+    if (b.prefix[m + 1] <= c0) {          // the last tensor that begins at c0 or before (one by one, us: clipping 512 tensors of 3 million elements 31 and 16, of 12 million 44 and 33)
+        for (int end = b.count - 1; m < end;) {
+            const int mid = (m + end + 1) >> 1;
+            if (b.prefix[mid] <= c0) m = mid;
+            else end = mid - 1;
+        }
+    }
     for (int k = m; k < b.count && b.prefix[k] < c1; ++k) {
         const unsigned first = b.prefix[k];
         const unsigned long long from = c0 > first ? (unsigned long long)(c0 - first) * GN_CHUNK : 0;
