@@ -347,7 +347,7 @@ constexpr int SPLIT_PRODUCTS = 8;
 constexpr int split_a(int e) { return e < 2 ? e + 1 : e < 5 ? e - 2 : e < 7 ? e - 5 : 0; }       // 1 2 0 1 2 0 1 0
 constexpr int split_b(int e) { return e < 2 ? 2 - e : e < 5 ? 4 - e : e < 7 ? 6 - e : 0; }       // 2 1 2 1 0 1 0 0
 
-// One tile.  KIND 0: bf16, 1: fp16, 2: fp32.  STREAM: results of whole cache lines to a row, which go past the caches (factor_expert.h).
+// One tile.  KIND 0: bf16, 1: fp16, 2: fp32.  STREAM: results of whole halves of cache lines to a row, which go past the caches (factor_expert.h).
 template <int TW, int KIND, int FEED, bool DIAG, bool STREAM = false>
 __device__ __forceinline__ void factor_tile_run(const View& v, const KFAC_AS1 unsigned char* x, const TileJob& job,
                                                 const OutSpec& os, unsigned char* smem) {

@@ -1,7 +1,7 @@
 // The norm over the gradients of many tensors, and clipping by it:
 //     norm = sqrt(sum g^2),   out = g min(1, max_norm / norm).
 // HBM bound: a gradient's bytes once for the norm, twice more for the clipping.  Launches:
-//   grad_partial_kernel   up to NORM_WGS workgroups in all, each a run of consecutive 4096-element chunks; a double each
+//   grad_partial_kernel   up to NORM_WGS workgroups, each some steps of one or several 4096-element chunks; a double each
 //   grad_norm_kernel      (the norm alone) adds those up
 //   grad_clip_kernel      every workgroup adds them up itself, in the same order, which saves the launch between
 // Squares are added in double precision: fp32 squares of bf16 or fp32 gradients beyond 1.8e19 overflow, and those below 1e-23 vanish.
