@@ -124,8 +124,8 @@ def test_more_than_four_gigabytes_in_one_tensor():
     assert bool((g[:-3] == 0.25).all()) and g[-3:].tolist() == [0.5] * 3     # (1 / 4 and a scale within 2 u of it round alike)
 
 
-def test_captured_and_replayed():
-    sizes = [30000, 1, 500, 77777]
+@pytest.mark.parametrize("sizes", [[30000, 1, 500, 77777], [1 + 37 * i for i in range(300)], [1 + i % 11 for i in range(1100)]], ids=len)
+def test_captured_and_replayed(sizes):
     a, b = grads(sizes, [F32, BF16], 0), grads(sizes, [F32, BF16], 0)
     out_a, out_b = [torch.zeros_like(t) for t in a], [torch.zeros_like(t) for t in b]
     one, two = kb.GradBatch(a, out_a), kb.GradBatch(b, out_b)
