@@ -7,7 +7,8 @@
 // the last range end.  Ranges of all experts, tiles inside a range, are one work list, of which every XCD gets a contiguous part, so that the tiles of a
 // range, which read the same rows, share an L2 (tiles of 2, 4 and 8 ranges in turns: 387 -> 502, 634 and 534 us): an eighth of the units, or, where they take
 // several rounds, of the work (equal numbers of experts of unequal rows left XCDs waiting: 65,536 rows of 2,048 columns, 32 experts of softmax(0.5 z) and
-// softmax(2 z) of them, 375 -> 341 and 574 -> 409 us; of equal experts 330 and 337).
+// softmax(2 z) of them, 375 -> 341 and 574 -> 409 us; of equal experts 330 and 337), the longest ranges first, so that none begins when the others end (343 -> 324
+// and 413 -> 389, of equal experts 342 and 339; 64 of 1,024 columns and softmax(z) of the rows 138 -> 122).
 // An expert of one range goes straight to its destination; the others' partial sums are added up by a second launch, which there is if
 // an expert can have more than rows_per rows at all.
 // Addresses.  A workgroup takes its range's first row for the tensor's beginning and its last one for the end: offsets inside it fit 32 bits
@@ -64,7 +65,8 @@ __device__ __forceinline__ T wave_scan(T v) {
 
 // Of the ranges of all experts (SPLIT: of the experts of several ranges) the one that `pick` names (-1: none).  False: none.
 // Every wavefront works it out by itself, some experts to a lane: without LDS and barriers.  pick(all, units_before): the number of ranges, and a function that
-// tells how many of their tiles lie before a fraction of all the work (experts' rows and `beside` for each range; a lane's experts count as alike).
+// tells how many of their tiles lie before a fraction of all the work (experts' rows and `beside` for each range; a lane's experts count as alike), and
+// one that gives number `at` of the tiles lo .. hi - 1 in the order of their ranges' rows, the longest first (by a lane's longest).
 template <bool SPLIT, class Pick>
 __device__ __forceinline__ bool expert_range(const ExpertArgs& a, Pick&& pick, ExpertRange& out) {
     const int lane = threadIdx.x & 63, per = (a.experts + 63) >> 6, e0 = lane * per, e1 = min(e0 + per, a.experts);
@@ -76,7 +78,7 @@ __device__ __forceinline__ bool expert_range(const ExpertArgs& a, Pick&& pick, E
     unsigned key = 0, part = 0;                                        // of this lane's experts
     int row = 0, rows = 0;                                             // of the last of them
     unsigned n = 0;
-    int there_rows = 0;
+    int there_rows = 0, largest = 0;                                   // of this lane's ranges
     auto take = [&](int from, int to) {
         expert_rows(a, from, to, row, rows);
         n = ranges_of(rows);
@@ -90,6 +92,7 @@ __device__ __forceinline__ bool expert_range(const ExpertArgs& a, Pick&& pick, E
         key += SPLIT ? (n > 1) : n;
         part += n > 1 ? n : 0;
         there_rows += rows;
+        largest = max(largest, min(rows, a.rows_per));
     }
     unsigned k = wave_scan(key), p = wave_scan(part);
     unsigned all = (unsigned)__builtin_amdgcn_readlane((int)k, 63);
@@ -105,7 +108,18 @@ __device__ __forceinline__ bool expert_range(const ExpertArgs& a, Pick&& pick, E
         const unsigned tiles = key * a.ntiles, mine = (k - key) * a.ntiles + min((unsigned)(inside * (float)tiles), tiles);
         return min((unsigned)__builtin_amdgcn_readlane((int)mine, __builtin_amdgcn_readfirstlane(__ffsll(beyond) - 1)), all * a.ntiles);
     };
-    const int want = pick((int)all, units_before);                     // (the same in all lanes)
+    auto by_size = [&](unsigned lo, unsigned hi, unsigned at) -> int {
+        const unsigned begin = max((k - key) * a.ntiles, lo), end = min(k * a.ntiles, hi), here = end > begin ? end - begin : 0;   // this lane's of them
+        unsigned before = 0;
+        for (unsigned long long m = __ballot(here > 0); m; m &= m - 1) {
+            const int other = __builtin_amdgcn_readfirstlane(__ffsll(m) - 1), size = __builtin_amdgcn_readlane(largest, other);
+            const unsigned units = (unsigned)__builtin_amdgcn_readlane((int)here, other);
+            before += (size > largest) | ((size == largest) & (other < lane)) ? units : 0;
+        }
+        const unsigned long long mine = __ballot((at >= before) & (at - before < here));
+        return mine ? __builtin_amdgcn_readlane((int)(begin + at - before), __builtin_amdgcn_readfirstlane(__ffsll(mine) - 1)) : -1;
+    };
+    const int want = pick((int)all, units_before, by_size);            // (the same in all lanes)
     if (want < 0 || (unsigned)want >= all) return false;
     auto owner_of = [&]() { return __builtin_amdgcn_readfirstlane(__ffsll(__ballot((unsigned)want >= k - key && (unsigned)want < k)) - 1); };
     int owner = owner_of(), first = 0;
@@ -183,12 +197,13 @@ void expert_tile_kernel(ExpertArgs a) {
     constexpr int ES = KIND == 2 ? 4 : 2;
     ExpertRange r;
     int tile = 0;
-    const bool there = expert_range<false>(a, [&](int all, auto&& units_before) {
+    const bool there = expert_range<false>(a, [&](int all, auto&& units_before, auto&& by_size) {
         int unit;
         if (a.beside > 0.f) {                                          // workgroups k, k + 8, ..: the eighth of the work that XCD k gets
             const int xcd = blockIdx.x & 7;
-            unit = (int)((xcd ? units_before(0.125f * xcd) : 0) + (blockIdx.x >> 3));
-            if (unit >= (int)units_before(0.125f * (xcd + 1))) return -1;
+            const unsigned lo = xcd ? units_before(0.125f * xcd) : 0, hi = units_before(0.125f * (xcd + 1)), at = blockIdx.x >> 3;
+            unit = at < hi - lo ? by_size(lo, hi, at) : -1;
+            if (unit < 0) return -1;
         } else {
             unit = unit_of(all * a.ntiles, blockIdx.x, 0);
             if (unit < 0) return -1;

@@ -28,7 +28,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4, 8))) voi
     ExpertRange r;
     unsigned unit = 0, last = 0;
     int j = 0;
-    bool there = expert_range<true>(a, [&](int all, auto&&) {
+    bool there = expert_range<true>(a, [&](int all, auto&&, auto&&) {
         const unsigned units = (unsigned)all * (unsigned)per, each = units / gridDim.x, more = units - each * gridDim.x;
         unit = blockIdx.x * each + min(blockIdx.x, more);
         last = unit + each + (blockIdx.x < more);
@@ -39,7 +39,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4, 8))) voi
         if (in == (unsigned)per) {
             in = 0;
             ++j;
-            there = expert_range<true>(a, [&](int, auto&&) { return j; }, r);
+            there = expert_range<true>(a, [&](int, auto&&, auto&&) { return j; }, r);
         }
         if (there) {
             FactorPlan pl;
