@@ -8,7 +8,9 @@
 // range, which read the same rows, share an L2 (tiles of 2, 4 and 8 ranges in turns: 387 -> 502, 634 and 534 us): an eighth of the units, or, where they take
 // several rounds, of the work (equal numbers of experts of unequal rows left XCDs waiting: 65,536 rows of 2,048 columns, 32 experts of softmax(0.5 z) and
 // softmax(2 z) of them, 375 -> 341 and 574 -> 409 us; of equal experts 330 and 337), the longest ranges first, so that none begins when the others end (343 -> 324
-// and 413 -> 389, of equal experts 342 and 339; 64 of 1,024 columns and softmax(z) of the rows 138 -> 122).
+// and 413 -> 389, of equal experts 342 and 339; 64 of 1,024 columns and softmax(z) of the rows 138 -> 122).  Workgroups are as many as there can be units
+// in all, an eighth of them on every XCD; those that find none of their XCD's take what another has more (twice as many workgroups, of which most found
+// nothing, took 8 to 12 us of 340).
 // An expert of one range goes straight to its destination; the others' partial sums are added up by a second launch, which there is if
 // an expert can have more than rows_per rows at all.
 // Addresses.  A workgroup takes its range's first row for the tensor's beginning and its last one for the end: offsets inside it fit 32 bits
@@ -97,11 +99,10 @@ __device__ __forceinline__ bool expert_range(const ExpertArgs& a, Pick&& pick, E
     unsigned k = wave_scan(key), p = wave_scan(part);
     unsigned all = (unsigned)__builtin_amdgcn_readlane((int)k, 63);
     if (all > (unsigned)a.ranges) all = (unsigned)a.ranges;            // (offsets that do not ascend could name more)
-    // (With `beside` at least an average range's rows, an eighth of the work is at most a quarter of the units.)
     auto units_before = [&](float fraction) -> unsigned {
         const float some = wave_scan((float)there_rows), total = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, some), 63));
-        const float beside = max(a.beside, total / (float)max(all, 1u)), work = (float)there_rows + beside * (float)key;
-        const float upto = some + beside * (float)k, goal = (total + beside * (float)all) * fraction;
+        const float work = (float)there_rows + a.beside * (float)key;
+        const float upto = some + a.beside * (float)k, goal = (total + a.beside * (float)all) * fraction;
         const unsigned long long beyond = __ballot(upto > goal);
         if (!beyond || fraction >= 1.f) return all * a.ntiles;
         const float inside = work > 0.f ? max(goal - (upto - work), 0.f) / work : 0.f;
@@ -201,8 +202,28 @@ void expert_tile_kernel(ExpertArgs a) {
         int unit;
         if (a.beside > 0.f) {                                          // workgroups k, k + 8, ..: the eighth of the work that XCD k gets
             const int xcd = blockIdx.x & 7;
-            const unsigned lo = xcd ? units_before(0.125f * xcd) : 0, hi = units_before(0.125f * (xcd + 1)), at = blockIdx.x >> 3;
-            unit = at < hi - lo ? by_size(lo, hi, at) : -1;
+            const unsigned wgs = gridDim.x >> 3;                       // of an XCD
+            unsigned lo = units_before(0.125f * xcd), hi = units_before(0.125f * (xcd + 1)), at = blockIdx.x >> 3;
+            if (at >= hi - lo) {                                       // those without any take, in order, what is more than another XCD's workgroups
+                unsigned more = at - (hi - lo);
+                unsigned from = 0;
+                for (int y = 0; y < xcd; ++y) {
+                    const unsigned to = units_before(0.125f * (y + 1));
+                    more += to - from < wgs ? wgs - (to - from) : 0;
+                    from = to;
+                }
+                bool found = false;
+                for (int y = 0; y < 8 && !found; ++y) {
+                    lo = y ? hi : 0;
+                    hi = units_before(0.125f * (y + 1));
+                    const unsigned over = hi - lo > wgs ? hi - lo - wgs : 0;
+                    found = more < over;
+                    if (!found) more -= over;
+                }
+                if (!found) return -1;
+                at = wgs + more;
+            }
+            unit = by_size(lo, hi, at);
             if (unit < 0) return -1;
         } else {
             unit = unit_of(all * a.ntiles, blockIdx.x, 0);
@@ -217,7 +238,9 @@ void expert_tile_kernel(ExpertArgs a) {
         expert_zeros(as_global(a.dst) + (size_t)r.expert * a.result, a.result, tile, a.ntiles);
         return;
     }
-    const int first = r.sub * a.rows_per, count = min(a.rows_per, r.rows - first);
+    // The expert's ranges are alike, of whole slabs (65,536 rows, 2,048 columns, us, of rows_per and what is left, and alike: 4 experts 316 and 290, 8 370 and
+    // 348; 131,072 rows of 1,024, 16 equal experts 178 and 208, of softmax(z) 260 and 249).
+    const int each = (((unsigned)r.rows + r.ranges - 1) / (unsigned)r.ranges + 63) & ~63, first = r.sub * each, count = min(each, r.rows - first);
     const View v = expert_view(a, count, r.rows);
     TileJob job;
     tri_decode_blocked<4>(a.tiles_dim, tile, job.I, job.J);

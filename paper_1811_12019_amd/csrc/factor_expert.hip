@@ -183,13 +183,12 @@ extern "C" int kfac_expert_factor(const kfac_expert_factor_desc* desc, const voi
     a.ranges = (int)c.ranges;
     a.parts = (int)c.parts;
     a.streams = a.mode != OUT_PACKED && a.dout % 16 == 0 && (uintptr_t)dst % 64 == 0 && a.result * sizeof(float) * d.experts > EXPERT_STREAM;
-    // Where the tiles take several rounds, an XCD gets an eighth of their work and not of their number; it may then have twice as many (see
-    // units_before; and some, for what the fractions are rounded to), and workgroups that find nothing left end.
+    // Where the tiles take several rounds, an XCD gets an eighth of their work and not of their number.
     const long long most = c.ranges * c.ntiles;
-    const float beside = c.tw == 256 ? 1000.f : f32 ? 200.f : 400.f;
+    const float beside = c.tw == 256 ? 500.f : f32 ? 100.f : 300.f;
     const bool by_work = most > 2 * (c.tw == 256 ? 256 : f32 ? 512 : 768) && d.rows >= 0.5f * beside * c.ranges;   // (of few rows units are alike)
     a.beside = by_work ? beside : 0.f;
-    const long long wgs = by_work ? (most / 4 + 16) * 8 : (most + 7) / 8 * 8;
+    const long long wgs = (most + 7) / 8 * 8;
     // (Four workgroups to a part, which share out its rows and its sums, where there are many ranges to an expert and few parts: 64 columns, 4 experts
     // of 16 ranges 15.0 -> 13.4 us, 192 columns, 2 of 10 16.5 -> 14.9; 256 columns, 8 of 8, 384 parts, 23.8 and 26.8.)
     const int groups = d.rows / d.experts >= 4 * c.rows_per && (long long)d.experts * c.ntiles * (c.tw / 32) * (c.tw / 32) <= 256 ? 4 : 1;
