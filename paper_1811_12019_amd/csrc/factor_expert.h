@@ -5,8 +5,8 @@
 // known on the device only.  A launch has workgroups for the most there can be: rows / rows_per whole ones and a part for every expert, times
 // the tiles.  Every wavefront reads the offsets, adds up the ranges before each expert's (one scan in registers) and finds its own; those behind
 // the last range end.  Ranges of all experts, tiles inside a range, are one work list, of which every XCD gets a contiguous part, so that the tiles of a
-// range, which read the same rows, share an L2 (tiles of 2, 4 and 8 ranges in turns: 387 -> 502, 634 and 534 us): an eighth of the units, or, where they take
-// several rounds, of the work (equal numbers of experts of unequal rows left XCDs waiting: 65,536 rows of 2,048 columns, 32 experts of softmax(0.5 z) and
+// range, which read the same rows, share an L2 (tiles of 2, 4 and 8 ranges in turns: 387 -> 502, 634 and 534 us): an eighth of the units, or, where they are
+// not few, of the work (equal numbers of experts of unequal rows left XCDs waiting: 65,536 rows of 2,048 columns, 32 experts of softmax(0.5 z) and
 // softmax(2 z) of them, 375 -> 341 and 574 -> 409 us; of equal experts 330 and 337), the longest ranges first, so that none begins when the others end (343 -> 324
 // and 413 -> 389, of equal experts 342 and 339; 64 of 1,024 columns and softmax(z) of the rows 138 -> 122).  Workgroups are as many as there can be units
 // in all, an eighth of them on every XCD; those that find none of their XCD's take what another has more (twice as many workgroups, of which most found

@@ -183,10 +183,11 @@ extern "C" int kfac_expert_factor(const kfac_expert_factor_desc* desc, const voi
     a.ranges = (int)c.ranges;
     a.parts = (int)c.parts;
     a.streams = a.mode != OUT_PACKED && a.dout % 16 == 0 && (uintptr_t)dst % 64 == 0 && a.result * sizeof(float) * d.experts > EXPERT_STREAM;
-    // Where the tiles take several rounds, an XCD gets an eighth of their work and not of their number.
+    // Where the tiles may fill half the chip, an XCD gets an eighth of their work and not of their number (bf16, us, by number and by work: 16,384 rows, 32
+    // experts of 768 columns, equal and of softmax(1.5 z) of the rows, 34 and 35, 54 and 47; 32 of 512 22 and 22, 28 and 26; 20,000 rows, 40 of 256 11.9 and 12.3).
     const long long most = c.ranges * c.ntiles;
     const float beside = c.tw == 256 ? 500.f : f32 ? 100.f : 300.f;
-    const bool by_work = most > 2 * (c.tw == 256 ? 256 : f32 ? 512 : 768) && d.rows >= 0.5f * beside * c.ranges;   // (of few rows units are alike)
+    const bool by_work = most > (c.tw == 256 ? 256 : f32 ? 512 : 768) / 2 && d.rows >= 0.5f * beside * c.ranges;   // (of few rows units are alike)
     a.beside = by_work ? beside : 0.f;
     const long long wgs = (most + 7) / 8 * 8;
     // (Four workgroups to a part, which share out its rows and its sums, where there are many ranges to an expert and few parts: 64 columns, 4 experts
