@@ -83,22 +83,21 @@ static bool expert_factor_ok(const kfac_expert_factor_desc* d) {
 // an average expert's rows and of 512: 71 experts of 572 rows, 624 columns 158 and 229, of softmax(0.8 z) 178 and 182; 40 of 700, 768 columns 152 and 205, of
 // softmax(0.3 z) 166 and 182, of softmax(0.8 z) 172 and 170; 64 of 781, 512 columns 130 and 159, 149 and 160, 162 and 150); calls of few rows need no second launch
 // (fp32, us, with one and with two: 18 experts' 1,187 rows of 59 columns 11.3 and 14.9, 9 experts' 1,045 of 114 13.3 and 15.4, 5 experts' 1,240 of 32 13.2 and 11.7).
-// Width: 64 where wider tiles would leave CUs without one or cover much more than the matrix, 256 from so many tile rows on that a workgroup
-// outlasts its epilogue, with little padding.
-// Both sides, bf16, us (128- and 256-wide at the rows of a range that suit each best; 64- and 128-wide):
-//     512 columns, 8 experts of 4,096 rows 34 and 40; 32 of 1,024 39 and 46; 32 of 4,096 95 and 77; 128 of 1,024 98 and 94
-//     1,024 columns, 8 of 1,024 36 and 45; 8 of 4,096 78 and 69; 32 of 256 52 and 53; 32 of 1,024 105 and 93; 128 of 64 113 and 119; of 256 156 and 141
-//     2,048 columns, 8 of 256 40 and 48; 8 of 1,024 90 and 86; 32 of 64 115 and 118; 32 of 256 168 and 147; 32 of 1,024 345 and 257
-//     fp32, 30 of 1,000 rows, 192 columns 31 and 39, 256 43 and 41, 320 58 and 64; 80 of 132 rows, 329 columns 48 and 44
-//     512 columns, 8 experts of 64 rows 8.3 and 10.4; of 256 10.3 and 12.4; 32 of 64 15.9 and 13.2; fp32, 256 columns, 8 of 256 16 and 21; 8 of 2,048 32 and 30
-// Rows of a range: 1,024 columns, 256 wide, 32 of 4,096 1,024 298, 2,048 246, 6,400 211; 8 of 4,096 86, 69, 111; 512 columns, 128 wide, 8 of 4,096
-// 1,024 36, 1,536 34; fp32, 1,024 columns, 8 of 1,024 256 108, 512 100, 1,024 118; 512 columns, 64 of 1,024 512 195, 1,024 200, 1,600 213.
+// Width: 64 where wider tiles would leave CUs without one or cover much more than the matrix, 256 where there are many tiles of many rows, so that a
+// workgroup outlasts its epilogue, with little padding.  Both sides, us:
+//     128- and 256-wide, bf16, equal experts, then softmax(0.5 z) of the rows: 512 columns, 32 experts of 4,096 rows 84 and 84, 85 and 88; 64 of 2,048 75 and 60,
+//     85 and 78; 1,024 columns, 8 of 4,096 74 and 60, 75 and 74; 32 of 1,024 62 and 70, 88 and 82; 64 of 512 72 and 86, 75 and 82; 2,048 columns, 8 of 1,024
+//     63 and 75, 69 and 75; 8 of 2,048 100 and 109, 106 and 109; 32 of 1,024 197 and 196, 267 and 218; 64 of 512 278 and 263, 370 and 301; 32 of 2,048 411 and 319
+//     64- and 128-wide: bf16, 512 columns, 8 experts of 64 rows 6.5 and 8.1; of 256 7.8 and 9.2; 32 of 64 12.8 and 11.8; fp32, 256 columns, 8 of 256 12 and 24; 8 of
+//     2,048 28 and 27; 30 of 1,000 rows, 192 columns 30 and 39, 256 42 and 42, 320 53 and 59; 80 of 132 rows, 329 columns 43 and 37
+// Rows of a range: 1,024 columns, 256 wide, 32 of 4,096 1,024 303, 2,048 256, 6,400 184; 8 of 4,096 81, 70, 85; 512 columns, 128 wide, 8 of 4,096
+// 1,024 31, 1,536 26; fp32, 1,024 columns, 8 of 1,024 256 105, 512 109, 1,024 124; 512 columns, 64 of 1,024 512 198, 1,024 195, 1,600 164.
 // Results in rows of whole halves of cache lines go past the caches where two of them do not stay in the 256 MB memory-side one (smaller parts of lines
 // written past them cost as much again: 8,192 rows of 64 experts, 1,000 columns 96 and 119, 1,025 109 and 154; 88 experts' 1,233 206 and 318).  bf16, us, kept and
 // past them: 8,192 rows, 64 experts of 1,024 columns (256 MB) 64 and 56, of 1,008 90 and 63, as running averages 118 and 91; 32 of 1,008 (124 MB) 57 and 39,
 // 67 and 57; 56 of 736 (116 MB) 26.7 and 29.7, 34.6 and 42.5; 16 of 2,000 columns, 16,384 rows 168 and 118, 179 and 148; fp32, 64 of 816 78 and 56, 82 and 76.
 constexpr size_t EXPERT_STREAM = (size_t)120 << 20;
-constexpr double FEW_WGS = 160, WIDE_TILE_ROWS = 200000;
+constexpr double FEW_WGS = 160, WIDE_TILE_ROWS = 150000, WIDE_WORK = 6e8;      // (rows of all tiles; times an expert's rows)
 
 static ExpertCut expert_cut(const kfac_expert_factor_desc& d) {
     ExpertCut c;
@@ -120,7 +119,8 @@ static ExpertCut expert_cut(const kfac_expert_factor_desc& d) {
     c.tw = 128;
     const double fit = 0.25 * tiles(64) / tiles(128);
     if (d.dim <= 64 || fit <= (f32 ? 0.7 : 0.55) || tiles(128) * d.experts * std::max(1.0, std::ceil(each / rows_of_width(128))) < FEW_WGS) c.tw = 64;
-    else if (!f32 && d.dim > 128 && 4 * tiles(256) <= WIDE_PADDING * tiles(128) && tiles(256) * rows >= WIDE_TILE_ROWS) c.tw = 256;
+    else if (!f32 && d.dim > 128 && 4 * tiles(256) <= WIDE_PADDING * tiles(128) && tiles(256) * rows >= WIDE_TILE_ROWS &&
+             tiles(256) * rows * each >= WIDE_WORK) c.tw = 256;
     c.rows_per = rows_of_width(c.tw);
     c.tiles_dim = ceil_div(d.dim, c.tw);
     c.ntiles = c.tiles_dim * (c.tiles_dim + 1) / 2;
