@@ -356,7 +356,8 @@ def test_factor_of_many_rows(rows, E, dim, dtype):
             check_factor(f64(S[e:e + 1]), f64(new)[None], ema=True)
 
 
-@pytest.mark.parametrize("rows,E,dim,dtype", [(60000, 60, 768, "bf16"), (60000, 90, 640, "f16"), (30000, 90, 384, "f32"), (60000, 700, 200, "bf16")])
+@pytest.mark.parametrize("rows,E,dim,dtype", [(60000, 60, 768, "bf16"), (60000, 90, 640, "f16"), (30000, 90, 384, "f32"), (60000, 700, 200, "bf16"),
+                                               (65536, 20, 1280, "bf16"), (40000, 14, 1536, "f16"), (65536, 70, 512, "bf16")])
 def test_factor_tiles_dealt_by_work(rows, E, dim, dtype):
     """More tiles than the chip takes in two rounds, of experts of few, of many and of all the rows, one and several experts to a lane of the
     search: every expert against the reference on the GPU in 64 bits."""
