@@ -79,8 +79,9 @@ static bool expert_factor_ok(const kfac_expert_factor_desc* d) {
 // Width of the tiles and rows of a range, from the call's rows and experts of equal size.  Rows: as many as let all ranges run in as few rounds of the
 // workgroups that fit the chip (768, of 256-wide tiles 256, fp32 512 and one round more) as uncut experts would, counting half a range for every expert's
 // end, and not so few that a second range costs a tile more in partial sums than it saves; ranges near an average expert's rows are made longer, so that
-// most experts are one (three times as long where there are workgroups enough to even out the long ones; fp32, us, ranges of 1.25 times
-// an average expert's rows and of 512: 71 experts of 572 rows, 624 columns 158 and 229, of softmax(0.8 z) 178 and 182; 40 of 700, 768 columns 152 and 205, of
+// most experts are one (three times as long where there are workgroups enough to even out the long ones: bf16, us, three and one and a half times, 32 experts of
+// 1,024 rows, 1,024 columns and softmax(z) 79 and 94, 128 of 512 and 512 columns 59 and 69; 32 of 2,048, 512 columns, uncut and cut 45 and 57; fp32, ranges of 1.25
+// times an average expert's rows and of 512: 71 experts of 572 rows, 624 columns 158 and 229, of softmax(0.8 z) 178 and 182; 40 of 700, 768 columns 152 and 205, of
 // softmax(0.3 z) 166 and 182, of softmax(0.8 z) 172 and 170; 64 of 781, 512 columns 130 and 159, 149 and 160, 162 and 150); calls of few rows need no second launch
 // (fp32, us, with one and with two: 18 experts' 1,187 rows of 59 columns 11.3 and 14.9, 9 experts' 1,045 of 114 13.3 and 15.4, 5 experts' 1,240 of 32 13.2 and 11.7).
 // Width: 64 where wider tiles would leave CUs without one or cover much more than the matrix, 256 where there are many tiles of many rows, so that a
@@ -111,8 +112,9 @@ static ExpertCut expert_cut(const kfac_expert_factor_desc& d) {
     auto tiles = [&](int tw) { const double n = ceil_div(d.dim, tw); return 0.5 * n * (n + 1); };
     auto rows_of_width = [&](int tw) {
         const double slots = tw == 256 ? 256 : f32 ? 512 : 768, whole = tiles(tw) * d.experts, rounds = std::max(std::ceil(whole / slots), 1.0) + f32;
-        double r = std::max(rows * tiles(tw) / (0.95 * rounds * slots - 0.5 * whole), !f32 ? 1024.0 : tw == 64 ? 128.0 : whole < slots ? 256.0 : 512.0);
-        if (r > 0.6 * each && (!f32 || whole >= slots)) r = std::max(r, (f32 ? 1.25 : whole >= 2 * slots ? 3 : 1.5) * each);
+        double r = std::max(rows * tiles(tw) / (0.95 * rounds * slots - 0.5 * whole), !f32 ? 1024.0 : whole < slots ? 256.0 : 512.0);
+        const bool many = whole >= (tw == 256 ? 1.5 : 0.75) * slots;
+        if (r >= (whole >= 0.25 * slots ? 0.5 : 0.6) * each && (!f32 || many)) r = std::max(r, (f32 ? 1.25 : many ? 3 : 1.5) * each);
         if (rows <= (f32 ? ROWS_PER_WG_MAX_F32 : 2048) && (tw == 64 || !f32)) r = std::max(r, rows);
         return (int)(std::min(r, (double)(f32 ? ROWS_PER_WG_MAX_F32 : ROWS_PER_WG_MAX)) + 63) / 64 * 64;
     };
