@@ -133,3 +133,26 @@ def test_a_captured_layer():
         torch.cuda.synchronize()
         for name in ("xs", "y", "dys", "dweights", "A_run", "G_run", "A_inv", "P", "norm"):
             assert torch.equal(getattr(one, name), getattr(two, name)), (seed, name)
+
+
+@pytest.mark.parametrize("T,K,E,d_in,d_out,dtype", [(0, 2, 3, 16, 8, torch.bfloat16), (1, 1, 1, 1, 1, torch.float32), (1, 64, 2, 8, 9, torch.float16),
+                                                    (5, 3, 64, 33, 7, torch.bfloat16), (7, 1, 1, 100, 50, torch.bfloat16)])
+def test_smallest_layers(T, K, E, d_in, d_out, dtype):
+    """No token, one, one expert, more experts than tokens, the same expert again and again: every call runs, and what it does not reach stays."""
+    g = torch.Generator(device=DEV).manual_seed(T + E)
+    layer = KfacExpertStep(T, K, E, d_in, d_out, dtype, max_norm=1.0)
+    expert = torch.randint(0, E, (T, K), generator=g, device=DEV, dtype=torch.int32)
+    x, dy = (torch.randn((T, d), generator=g, device=DEV).to(dtype) for d in (d_in, d_out))
+    ys, w = torch.randn((T * K, d_out), generator=g, device=DEV).to(dtype), torch.rand((T, K), generator=g, device=DEV)
+    half = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11, torch.float32: 2.0 ** -24}[dtype]
+    xs = layer.dispatch(expert, x)
+    offsets, order, place = eo.expert_sort(expert.cpu().numpy(), E)
+    np.testing.assert_array_equal(layer.route.offsets.cpu().numpy(), offsets)
+    near(layer.combine(ys, w), eo.expert_combine(f64(ys), f64(w), place, d_out), 2 * half + K * 2.0 ** -24)
+    dys, _ = layer.backward(dy, ys, w)
+    layer.gradW.normal_(generator=g)
+    P = layer.step()
+    assert layer.inverses.info.tolist() == [0] * (2 * E)
+    for t, run in ((xs, layer.A_run), (dys, layer.G_run)):
+        near(run, eo.expert_factor(f64(t), offsets, running=np.stack([np.eye(run.shape[1])] * E), decay=layer.decay), 2e-5)
+    assert bool(torch.isfinite(P).all()) and float(P.norm()) <= 1 + 2.0 ** -20
