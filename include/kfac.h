@@ -202,11 +202,11 @@ int kfac_weight_update_batched(const kfac_update_item* items_host, int32_t count
 
 /* The step between gradients and their update: the norm over all tensors, and clipping by it.
  * kfac_grad_norm_batched: *norm (device float) = sqrt(sum of g^2 over all elements of all items), summed in double precision, so that no
- * finite gradient's square overflows or vanishes; a norm beyond the largest float is given as infinity.
+ * finite gradient's square overflows or vanishes; a norm that rounds beyond the largest float is given as infinity.
  * kfac_grad_clip_batched: out = g * min(1, max_norm / norm), each element multiplied in fp32 by the scale rounded to fp32 and rounded to
  * its type once.  With given_norm = NULL the norm is that of the items, and is written to `norm` as well (ws as for kfac_grad_norm_batched);
  * else it is read from the device float given_norm (the norm over all processes; what it was computed from is the caller's), `norm` must
- * be NULL, and ws is not used.  A norm that is not finite leaves the gradients as they are (`norm` tells).  A scale of 1 writes nothing
+ * be NULL, and ws is not used.  A norm that is not finite, as a float, leaves the gradients as they are (`norm` tells).  A scale of 1 writes nothing
  * in place.  Items may differ in every field; those of no elements are skipped; tensors need their elements' alignment only.
  * max_norm >= 0.  Tensors that are written must not overlap others.  Deterministic: the same items give the same bits. */
 typedef struct kfac_grad_item {

@@ -7,7 +7,8 @@ Plain numpy, assignment by assignment, from the definitions:
   * dispatch: xs[place[i]] = x[t];  combine: y[t] = sum_k w[t, k] ys[place[t, k]];  their gradients;
   * the experts' Kronecker factors: F_e = scale * sum over expert e's rows of abar abar^T, abar the row with a trailing 1 if it
     has a bias, scale 1 / (its rows) unless given, 0 without rows; S_e <- decay S_e + (1 - decay) F_e, S_e as it was without rows;
-  * norm = sqrt(sum g^2) over all tensors, out = g min(1, max_norm / norm), g itself if the norm is not finite.
+  * norm = sqrt(sum g^2) over all tensors, infinite if it rounds beyond the largest float; out = g min(1, max_norm / norm), g itself if
+    the norm is not finite.
 """
 from __future__ import annotations
 
@@ -80,7 +81,8 @@ def expert_factor(x, offsets, has_bias=False, scale: float = 0.0, running=None, 
 
 
 def grad_norm(grads) -> float:
-    return float(np.sqrt(sum(float(np.sum(np.asarray(g, dtype=np.float64) ** 2)) for g in grads)))
+    norm = float(np.sqrt(sum(float(np.sum(np.asarray(g, dtype=np.float64) ** 2)) for g in grads)))
+    return np.inf if norm >= 2.0 ** 128 - 2.0 ** 103 else norm               # (half a step beyond the largest float)
 
 
 def grad_clip(grads, max_norm: float, norm=None):

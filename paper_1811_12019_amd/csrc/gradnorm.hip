@@ -156,7 +156,8 @@ __global__ __launch_bounds__(256) void grad_clip_kernel(GradBatch<MAX> b, const 
         len = sqrt(sum_of(partial, n, red));
         if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)len;
     }
-    const float scale = len > (double)max_norm && len < __builtin_inf() ? (float)((double)max_norm / len) : 1.f;
+    // (finite: as the float that the caller sees)
+    const float scale = len > (double)max_norm && (float)len < __builtin_inff() ? (float)((double)max_norm / len) : 1.f;
     const unsigned chunks = b.prefix[b.count];
     const unsigned c0 = (gridDim.x - 1 - blockIdx.x) * b.step;           // (what the first pass read last comes first)
     int m = tensor_of(b, c0);

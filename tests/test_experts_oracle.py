@@ -94,3 +94,12 @@ def test_a_norm_that_is_not_finite_clips_nothing():
     for bad in (np.nan, np.inf):
         out, norm = eo.grad_clip([np.array([1.0, bad])], 0.5)
         assert not np.isfinite(norm) and out[0][0] == 1.0
+
+
+def test_a_norm_beyond_the_largest_float_clips_nothing():
+    top = float(np.finfo(np.float32).max)
+    out, norm = eo.grad_clip([np.array([top, top])], 0.5)
+    assert norm == np.inf and out[0].tolist() == [top, top]
+    assert eo.grad_norm([np.array([top, top])]) == np.inf
+    out, norm = eo.grad_clip([np.array([top, 1e30])], top / 2)                    # rounds to the largest float
+    assert np.isfinite(norm) and out[0][0] == top / 2

@@ -164,3 +164,30 @@ def test_deterministic(dtype):
     first = kb.kfac_grad_norm_batched(batch).clone()
     for _ in range(3):
         assert torch.equal(kb.kfac_grad_norm_batched(batch), first)
+
+
+@pytest.mark.parametrize("into", ["place", "others"])
+@pytest.mark.parametrize("sizes,dtype", [([4], F32), ([5, 1, 300], BF16), ([1] * 600, F32), ([70000], BF16)], ids=lambda v: str(v)[:24])
+def test_a_norm_beyond_the_largest_float_clips_nothing(sizes, dtype, into):
+    """Finite gradients whose norm is no float: given as infinity, which clips nothing, whether computed in the call or handed to it."""
+    tensors = [torch.full((n,), 3e38, dtype=dtype, device=DEV) for n in sizes]
+    before = [t.clone() for t in tensors]
+    out = None if into == "place" else [torch.zeros_like(t) for t in tensors]
+    batch = kb.GradBatch(tensors, out)
+    norm = kb.kfac_grad_norm_batched(batch).clone()
+    assert float(norm) == float("inf")
+    used = kb.kfac_grad_clip_batched(batch, 1.0)
+    assert float(used) == float("inf")
+    assert all(torch.equal(a, b) for a, b in zip(tensors if out is None else out, before))
+    kb.kfac_grad_clip_batched(batch, 1.0, norm)
+    assert all(torch.equal(a, b) for a, b in zip(tensors if out is None else out, before))
+
+
+def test_the_largest_norm_that_is_a_float():
+    """A norm that rounds to the largest float clips as any other."""
+    top = float(np.finfo(np.float32).max)
+    tensors = [torch.tensor([top], device=DEV), torch.tensor([1e30], device=DEV)]
+    before = [t.clone() for t in tensors]
+    norm = kb.kfac_grad_clip_batched(kb.GradBatch(tensors), 1e38)
+    assert float(norm) == top
+    check(tensors, norm, before, 1e38)
