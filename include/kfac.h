@@ -223,7 +223,7 @@ int kfac_grad_clip_batched(const kfac_grad_item* items_host, int32_t count, floa
 
 /* Layers of experts.  Each of `tokens` tokens goes to `choices` of `experts` experts; an expert's Kronecker factors are built from its own
  * tokens, which are brought into the experts' order first.  Where they go is decided on the device, so that nothing here needs a
- * row count on the host. */
+ * row count on the host.  What is written must not overlap what else a call is given; rows may lie in the gaps between others' rows. */
 typedef struct kfac_expert_desc {
     int32_t tokens;      /* T >= 0; T * choices < 2^31 */
     int32_t choices;     /* K, 1 .. 64 */

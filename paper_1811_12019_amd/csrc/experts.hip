@@ -441,12 +441,24 @@ static int row_args(const kfac_expert_desc* d, RowArgs* a) {
 
 static bool on_grid(const void* p, size_t align) { return p && (uintptr_t)p % align == 0; }
 
-// Whether two tensors of rows may share elements (rows with gaps may lie in each other's).
+// Whether two tensors of np and nq rows of `row` bytes, ldp and ldq bytes from one to the next, share any.  (Rows with gaps may lie in each other's; with
+// gaps of two kinds that is not looked into.)
 static bool rows_overlap(const void* p, long long np, long long ldp, const void* q, long long nq, long long ldq, long long row) {
-    const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
-    if (a == b) return true;
-    if (ldp != row || ldq != row) return false;
-    return a < b + (uintptr_t)(nq * row) && b < a + (uintptr_t)(np * row);
+    const long long apart = (long long)((uintptr_t)q - (uintptr_t)p);
+    if (np == 1) ldp = row;
+    if (nq == 1) ldq = row;
+    const long long end_p = (np - 1) * ldp + row, end_q = (nq - 1) * ldq + row;
+    if (apart >= end_p || -apart >= end_q) return false;
+    if (ldp == row) {                                         // the first of q's rows that ends behind p's beginning
+        const long long j = apart + row > 0 ? 0 : -(apart + row) / ldq + 1;
+        return apart + j * ldq < end_p;
+    }
+    if (ldq == row) return rows_overlap(q, nq, ldq, p, np, ldp, row);
+    if (ldp != ldq) return apart == 0;
+    // Row j of q begins `in` bytes behind the place of p's row first + j.
+    const long long in = (apart % ldp + ldp) % ldp, first = (apart - in) / ldp;
+    auto meet = [&](long long i) { return i < np && i + nq > 0; };
+    return (in < row && meet(first)) || (ldp - in < row && meet(first + 1));
 }
 
 }  // namespace kfac

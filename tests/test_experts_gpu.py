@@ -543,3 +543,17 @@ def test_captured_and_replayed_on_another_stream():
     torch.cuda.synchronize()
     for name in outs:
         assert torch.equal(a[name], want[name]) and torch.equal(b[name], want[name]), name
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_side_by_side_in_one_buffer(dtype):
+    """Tensors whose rows lie in each other's gaps, without a common element, are apart."""
+    T, K, E, D = 90, 3, 4, 72
+    route, _ = routed(T, K, E, 0.1, 5)
+    dy, w = rows_of(T, D, TYPES[dtype], 0, 1), torch.rand((T, K), device=DEV)
+    apart = [rows_of(T * K, D, TYPES[dtype], 0, 2), torch.full((T * K, D), 5.0, dtype=TYPES[dtype], device=DEV)]
+    both = torch.cat(apart, 1)
+    dw = [torch.zeros((T, K), device=DEV) for _ in range(2)]
+    kb.kfac_expert_combine_backward(route, dy, apart[0], w, apart[1], dw[0])
+    kb.kfac_expert_combine_backward(route, dy, both[:, :D], w, both[:, D:], dw[1])
+    assert torch.equal(both, torch.cat(apart, 1)) and torch.equal(dw[0], dw[1])

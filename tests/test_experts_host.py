@@ -187,3 +187,26 @@ def test_binding_refuses_host_memory():
         kb.ExpertRoute(4, 2, 3, device="cpu")
     with pytest.raises(kb.KfacError):
         kb.ExpertFactors(4, 2, 3, torch.float32, device="cpu")
+
+
+def test_rows_with_gaps_that_overlap_are_refused():
+    """Written rows that share an element with rows that are read, whatever lies between the rows of either."""
+    lib = kb.load_library()
+    # 8 tokens, 16 rows of 64 bfloat16 (128 bytes); rows `ld` elements apart
+    def dispatch(ld_token, ld_row, off):
+        d = desc(ld_token=ld_token, ld_row=ld_row)
+        return lib.kfac_expert_dispatch(ctypes.byref(d), A, C, P(0x1000000 + off), None)
+
+    refused = [(128, 0, 0), (128, 0, 126), (128, 0, 7 * 256), (128, 0, 7 * 256 + 126), (128, 0, -2046),     # tokens with gaps, rows without
+               (0, 128, 126), (0, 128, 2), (0, 128, -15 * 256), (0, 128, -15 * 256 - 126),                  # rows with gaps, tokens without
+               (128, 128, 126), (128, 128, 256), (128, 128, 130), (128, 128, 7 * 256), (128, 128, 7 * 256 + 126), (128, 128, -126),   # both, as far apart
+               (128, 128, -15 * 256 - 126), (128, 128, -3 * 256 + 2), (192, 192, 64), (192, 192, -384 - 100)]
+    for ld_token, ld_row, off in refused:
+        assert dispatch(ld_token, ld_row, off) == INVALID, (ld_token, ld_row, off)
+    wide = ctypes.byref(desc(ld_token=128, ld_row=128, ld_grad=128))
+    near = P(0x2000000 + 64)
+    assert lib.kfac_expert_combine(wide, A, None, C, P(0x1000000 + 64), None) == INVALID
+    assert lib.kfac_expert_combine_backward(wide, A, B, None, C, P(0x1000000 + 256 - 2), None, None) == INVALID
+    assert lib.kfac_expert_combine_backward(wide, A, B, None, C, near, D, None) == INVALID
+    one = ctypes.byref(desc(tokens=1, choices=1, ld_token=128, ld_row=4096))                                # one row each: gaps are of no matter
+    assert lib.kfac_expert_dispatch(one, A, C, P(0x1000000 + 126), None) == INVALID
