@@ -268,7 +268,8 @@ typedef struct kfac_expert_factor_desc {
     int32_t dtype;       /* kfac_dtype of x */
     int32_t has_bias;
     int32_t packed;      /* 1: `out` receives packed upper triangles (kfac_pack_upper_batched) */
-    int64_t ld;          /* elements from one row to the next; 0: dim.  Rows that do not all begin at 16-byte addresses are copied first */
+    int64_t ld;          /* elements from one row to the next; 0: dim.  Whole 16-byte vectors (up to 2^18 elements): rows are read as they lie, in
+                            whole vectors, and x must be 16-byte aligned.  Else rows are copied first, and x needs its elements' alignment only */
 } kfac_expert_factor_desc;
 
 size_t kfac_expert_factor_workspace_bytes(const kfac_expert_factor_desc* desc);

@@ -665,8 +665,8 @@ def kfac_expert_combine_backward(route: ExpertRoute, dy: torch.Tensor, ys: Optio
 
 class ExpertFactors:
     """Descriptor and scratch of the factor builds of one layer of experts (built once, reused every step): x of `rows` rows of `dim`
-    elements of a torch dtype in the experts' order, `ld` elements from one row to the next (0: dim).  Calls that use one object must
-    not overlap in time."""
+    elements of a torch dtype in the experts' order, `ld` elements from one row to the next (0: dim).  Where these are whole 16-byte vectors x
+    has to be 16-byte aligned; others are copied first.  Calls that use one object must not overlap in time."""
 
     def __init__(self, rows: int, experts: int, dim: int, dtype: torch.dtype, has_bias: bool = False, packed: bool = False, ld: int = 0,
                  device="cuda"):
@@ -677,6 +677,7 @@ class ExpertFactors:
         self.d = self.dim + int(bool(has_bias))
         self.shape = (self.experts, packed_elems(self.d)) if packed else (self.experts, self.d, self.d)
         self.desc = kfac_expert_factor_desc(self.rows, self.experts, self.dim, _KFAC_DTYPE[dtype], int(bool(has_bias)), int(bool(packed)), int(ld))
+        self.on_grid = self.ld * dtype.itemsize % 16 == 0 and self.ld <= 1 << 18           # rows are read as they lie, not copied first
         self.ws = alloc_workspace(int(load_library().kfac_expert_factor_workspace_bytes(ctypes.byref(self.desc))), self.device)
         self.ws_bytes = 0 if self.ws is None else self.ws.numel()
 
@@ -688,6 +689,8 @@ def kfac_expert_factor(plan: ExpertFactors, x: torch.Tensor, offsets: torch.Tens
     if not (x.dtype == plan.dtype and x.shape == (plan.rows, plan.dim) and x.get_device() == plan.index and
             (plan.dim == 1 or x.stride(1) == 1) and (plan.rows <= 1 or x.stride(0) == plan.ld)):
         _want(False, where, f"x: {plan.dtype} of shape {(plan.rows, plan.dim)} on {plan.device}, rows {plan.ld} elements apart")
+    if plan.on_grid and x.data_ptr() % 16 and plan.rows:
+        _want(False, where, f"x: rows {plan.ld} elements apart, which are whole 16-byte vectors, have to begin at 16-byte addresses")
     if not (offsets.dtype == torch.int32 and offsets.shape == (plan.experts + 1,) and offsets.is_contiguous() and offsets.get_device() == plan.index):
         _want(False, where, f"offsets: {plan.experts + 1} contiguous int32 on {plan.device}")
     _want((out is None) != (running is None), where, "either out or running")

@@ -557,3 +557,24 @@ def test_rows_side_by_side_in_one_buffer(dtype):
     kb.kfac_expert_combine_backward(route, dy, apart[0], w, apart[1], dw[0])
     kb.kfac_expert_combine_backward(route, dy, both[:, :D], w, both[:, D:], dw[1])
     assert torch.equal(both, torch.cat(apart, 1)) and torch.equal(dw[0], dw[1])
+
+
+def test_factor_of_rows_off_the_16_byte_grid():
+    """Rows of whole vectors are read as they lie and have to begin on the grid: the refusal says so.  Others are copied, wherever they begin."""
+    bf, rows, E = torch.bfloat16, 12, 3
+    base = torch.randn(rows * 16 + 4, device=DEV).to(bf)
+    offsets = torch.tensor([0, 5, 5, 12], dtype=torch.int32, device=DEV)
+    plan = kb.ExpertFactors(rows, E, 16, bf)
+    out = torch.empty(plan.shape, device=DEV)
+    for at in (1, 4):
+        with pytest.raises(kb.KfacError, match="16-byte") as e:
+            kb.kfac_expert_factor(plan, base[at:at + rows * 16].view(rows, 16), offsets, out=out)
+        assert e.value.status == kb.KFAC_ERR_INVALID_ARG
+    kb.kfac_expert_factor(plan, base[:rows * 16].view(rows, 16), offsets, out=out)
+    check_factor(f64(out), eo.expert_factor(f64(base[:rows * 16].view(rows, 16)), offsets.tolist()))
+    odd = kb.ExpertFactors(rows, E, 15, bf)
+    out = torch.empty(odd.shape, device=DEV)
+    for at in (0, 1, 4):
+        x = base[at:at + rows * 15].view(rows, 15)
+        kb.kfac_expert_factor(odd, x, offsets, out=out)
+        check_factor(f64(out), eo.expert_factor(f64(x), offsets.tolist()))
