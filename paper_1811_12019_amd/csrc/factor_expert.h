@@ -288,8 +288,15 @@ int launch_expert_tiles(const ExpertArgs& a, unsigned wgs, hipStream_t stream)
         if (a.tw == 256 && a.streams) return launch_expert_tile_kernel<256, KIND, true>("expert_tile_kernel<256, 16-bit, stream>", a, wgs, stream);
         if (a.tw == 256) return launch_expert_tile_kernel<256, KIND, false>("expert_tile_kernel<256, 16-bit>", a, wgs, stream);
     }
-    if (a.streams) return launch_expert_tile_kernel<128, KIND, true>(KIND == 2 ? "expert_tile_kernel<128, f32, stream>" : "expert_tile_kernel<128, 16-bit, stream>", a, wgs, stream);
-    return launch_expert_tile_kernel<128, KIND, false>(KIND == 2 ? "expert_tile_kernel<128, f32>" : "expert_tile_kernel<128, 16-bit>", a, wgs, stream);
+    const bool narrow = a.tw == 64;                                    // (the kernel for 128-wide tiles has both; timed apart)
+    if (a.streams) {
+        const char* name = KIND == 2 ? narrow ? "expert_tile_kernel<64, f32, stream>" : "expert_tile_kernel<128, f32, stream>"
+                                     : narrow ? "expert_tile_kernel<64, 16-bit, stream>" : "expert_tile_kernel<128, 16-bit, stream>";
+        return launch_expert_tile_kernel<128, KIND, true>(name, a, wgs, stream);
+    }
+    const char* name = KIND == 2 ? narrow ? "expert_tile_kernel<64, f32>" : "expert_tile_kernel<128, f32>"
+                                 : narrow ? "expert_tile_kernel<64, 16-bit>" : "expert_tile_kernel<128, 16-bit>";
+    return launch_expert_tile_kernel<128, KIND, false>(name, a, wgs, stream);
 }
 template int launch_expert_tiles<KFAC_EXPERT_KIND>(const ExpertArgs&, unsigned, hipStream_t);
 #else

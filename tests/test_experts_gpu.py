@@ -578,3 +578,19 @@ def test_factor_of_rows_off_the_16_byte_grid():
         x = base[at:at + rows * 15].view(rows, 15)
         kb.kfac_expert_factor(odd, x, offsets, out=out)
         check_factor(f64(out), eo.expert_factor(f64(x), offsets.tolist()))
+
+
+@pytest.mark.parametrize("rows,E,dim,dtype,name", [(64, 2, 64, "bf16", "<64, 16-bit>"), (64, 2, 48, "f32", "<64, f32>"), (1024, 8, 256, "f32", "<64, f32>"),
+                                                   (20000, 200, 128, "f16", "<128, 16-bit>"), (20000, 200, 128, "f32", "<128, f32>"),
+                                                   (65536, 16, 768, "bf16", "<256, 16-bit>"), (21350, 854, 192, "bf16", "<64, 16-bit, stream>")])
+def test_timings_name_the_width_of_the_tiles(rows, E, dim, dtype, name):
+    plan = kb.ExpertFactors(rows, E, dim, TYPES[dtype])
+    x = torch.zeros((rows, dim), dtype=TYPES[dtype], device=DEV)
+    out = torch.empty(plan.shape, device=DEV)
+    offsets = torch.arange(E + 1, device=DEV).mul_(rows // E).to(torch.int32)
+    kb.kfac_kernel_timing_enable(True)
+    try:
+        kb.kfac_expert_factor(plan, x, offsets, out=out)
+        assert "expert_tile_kernel" + name in kb.kfac_kernel_timing_report()
+    finally:
+        kb.kfac_kernel_timing_enable(False)
