@@ -594,3 +594,104 @@ def test_timings_name_the_width_of_the_tiles(rows, E, dim, dtype, name):
         assert "expert_tile_kernel" + name in kb.kfac_kernel_timing_report()
     finally:
         kb.kfac_kernel_timing_enable(False)
+
+
+# ---- kernels that larger or longer calls take --------------------------------------------------------------------------
+@pytest.mark.parametrize("how", ["even", "skewed", "dropped", "one", "none"])
+@pytest.mark.parametrize("T,K,E", [(65536, 8, 256), (65535, 8, 256), (150000, 2, 64), (100001, 2, 700), (150001, 2, 1000), (150000, 2, 1000), (500000, 2, 37),
+                                   (499999, 2, 37), (500000, 2, 300), (800000, 2, 512), (1048576, 2, 64)])
+def test_sort_of_several_runs_of_several_steps(T, K, E, how):
+    """Runs of many workgroups whose wavefronts hold two to eight steps of assignments in registers, whole and cut; of 256 and more experts counted
+    several runs at a time."""
+    test_sort(T, K, E, how)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,K,E,D,gap,drop", [(700, 3, 5, 1001, 0, 0.1), (600, 2, 4, 1001, 6, 0.1), (513, 5, 9, 520, 0, 0.2)])
+def test_rows_of_several_vectors_to_a_lane(T, K, E, D, gap, drop, dtype):
+    """More tokens than a workgroup each is taken for, rows of 65 to 255 vectors: a wavefront goes over a token's row several times."""
+    test_dispatch(T, K, E, D, gap, drop, dtype)
+    test_combine(T, K, E, D, gap, drop, dtype, True)
+    test_combine_backward(T, K, E, D, gap, drop, dtype)
+
+
+def streaming(call):
+    """Runs `call` and says whether it took a kernel whose rows go past the caches."""
+    kb.kfac_kernel_timing_enable(True)
+    try:
+        call()
+        return all("stream>" in k for k in kb.kfac_kernel_timing_report())
+    finally:
+        kb.kfac_kernel_timing_enable(False)
+
+
+PAST_THE_CACHES = [(16384, 4, 64, 2048, "bf16"), (16300, 4, 64, 2001, "f16"), (9000, 7, 30, 1031, "f32"), (70000, 4, 16, 512, "bf16"), (300000, 2, 5, 128, "f32"),
+                   (430000, 4, 64, 64, "f16")]
+
+
+@pytest.mark.parametrize("T,K,E,D,dtype", PAST_THE_CACHES)
+def test_rows_past_the_caches(T, K, E, D, dtype):
+    """Calls that move more than 256 MB, whole and odd widths, some assignments dropped, against the same in 64 bits on the GPU."""
+    t = TYPES[dtype]
+    h = HALF[t]
+    g = torch.Generator(device=DEV).manual_seed(D)
+    expert = torch.randint(0, E, (T, K), generator=g, device=DEV, dtype=torch.int32)
+    expert[torch.rand((T, K), generator=g, device=DEV) < 0.05] = -1
+    route = kb.ExpertRoute(T, K, E)
+    kb.kfac_expert_sort(route, expert)
+    rows = int(route.offsets[E])
+    there, at = route.place >= 0, route.place.clamp(min=0).long()
+    x, ys, dy = rows_of(T, D, t, 0, 1), rows_of(T * K, D, t, 0, 2), rows_of(T, D, t, 0, 3)
+    ys[rows:] = float("nan")
+    w = torch.rand((T, K), generator=g, device=DEV) * 2 - 0.5
+    w[~there] = float("nan")
+    token = route.order[:rows].long() // K
+    xs, ok = guarded((T * K, D), t, 5.0)
+    assert streaming(lambda: kb.kfac_expert_dispatch(route, x, xs))
+    assert torch.equal(xs[:rows], x[token]) and bool((xs[rows:] == 5).all()) and ok()
+    del xs
+    for weights in (w, None):
+        y, ok = guarded((T, D), t, 5.0)
+        assert streaming(lambda: kb.kfac_expert_combine(route, ys, weights, y))
+        want, size = torch.zeros((T, D), dtype=torch.float64, device=DEV), torch.zeros((T, D), dtype=torch.float64, device=DEV)
+        for k in range(K):
+            term = ys[at[:, k]].double() * (1.0 if weights is None else w[:, k:k + 1].double())
+            term = torch.where(there[:, k:k + 1], term, 0.0)
+            want += term
+            size += term.abs()
+        assert bool(((y.double() - want).abs() <= K * U * size * (1 + h) + h * want.abs() + TINY[t]).all()) and ok()
+    for ask in (True, False):
+        dys, ok = guarded((T * K, D), t, 5.0)
+        dw = torch.full((T, K), float("nan"), device=DEV) if ask else None
+        assert streaming(lambda: kb.kfac_expert_combine_backward(route, dy, ys if ask else None, w, dys, dw))
+        want = dy[token].double() * w.reshape(-1)[route.order[:rows].long()].double()[:, None]
+        assert bool(((dys[:rows].double() - want).abs() <= (U + h) * want.abs() * (1 + h) + TINY[t]).all())
+        assert bool((dys[rows:] == 5).all()) and ok()
+        for k in range(K if ask else 0):
+            term = dy.double() * torch.where(there[:, k:k + 1], ys[at[:, k]].double(), 0.0)
+            assert bool(((dw[:, k].double() - term.sum(1)).abs() <= (D / 64 + 16) * U * term.abs().sum(1)).all())
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("rows,E,dim,gap,dtype", [(20000, 3, 60, 4, "bf16"), (20000, 3, 61, 2, "bf16"), (9000, 2, 130, 6, "f16"), (9000, 2, 300, 4, "bf16"),
+                                                  (8000, 2, 30, 2, "f32"), (8000, 2, 129, 3, "f32"), (7000, 2, 29, 2, "f32")])
+def test_factor_of_rows_with_gaps_in_several_ranges(rows, E, dim, gap, dtype, packed):
+    """Rows with NaN between them, a bias, and several ranges to an expert: the gaps are of no influence on sums and column sums."""
+    wide = rows_of(rows, dim + gap, TYPES[dtype], 0, dim)
+    wide[:, dim:] = float("nan")
+    x = wide[:, :dim]
+    for how in ("even", "uneven", "one"):
+        cut = bounds(rows, E, how, 1)
+        plan = kb.ExpertFactors(rows, E, dim, TYPES[dtype], has_bias=True, packed=packed, ld=dim + gap)
+        plan.ws.fill_(255)                                     # (NaN)
+        out = torch.empty(plan.shape, device=DEV)
+        kb.kfac_expert_factor(plan, x, torch.tensor(cut, dtype=torch.int32, device=DEV), out=out)
+        want = eo.expert_factor(f64(x), cut, True)
+        if packed:
+            i, j = np.triu_indices(dim + 1)
+            full = np.zeros_like(want)
+            full[:, i, j] = f64(out)
+            full[:, j, i] = f64(out)
+            check_factor(full, want)
+        else:
+            check_factor(f64(out), want)
