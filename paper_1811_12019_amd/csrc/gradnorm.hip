@@ -238,7 +238,8 @@ static size_t gn_bytes(const kfac_grad_item* items, int count) {
     return bytes;
 }
 
-// Workgroups, and sums, of the first pass's launch: all workgroups of the second one read them, at most 4096 of all launches.
+// Workgroups, and sums, of the first pass's launch: all workgroups of the second one read them, at most 4096 of up to 64 launches (32,768 tensors), and
+// 64 a launch of more.
 static unsigned norm_wgs(unsigned chunks, int count) {
     const unsigned launches = (unsigned)((count + GN_MAX - 1) / GN_MAX), steps = gn_steps(chunks);
     const unsigned most = launches <= 4 ? NORM_WGS : launches >= 64 ? 64 : 4096 / launches;

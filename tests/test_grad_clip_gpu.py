@@ -191,3 +191,15 @@ def test_the_largest_norm_that_is_a_float():
     norm = kb.kfac_grad_clip_batched(kb.GradBatch(tensors), 1e38)
     assert float(norm) == top
     check(tensors, norm, before, 1e38)
+
+
+def test_tensors_of_more_than_64_launches():
+    """Slices of one buffer, as many as take 66 launches, each of which then leaves fewer sums."""
+    sizes = [1 + i % 5 for i in range(65 * 512 + 77)]
+    flat = torch.randn(sum(sizes), generator=torch.Generator(device=DEV).manual_seed(1), device=DEV)
+    tensors = list(flat.split(sizes))
+    out = torch.zeros_like(flat)
+    batch = kb.GradBatch(tensors, list(out.split(sizes)))
+    norm = kb.kfac_grad_clip_batched(batch, 3.0)
+    check([out], norm, [flat], 3.0)
+    assert torch.equal(kb.kfac_grad_norm_batched(batch), norm)
