@@ -497,7 +497,8 @@ def _dense(t: torch.Tensor) -> bool:
 
 
 class GradBatch:
-    """A kfac_grad_item table (host memory; built once, reused every step), its scratch and the device float `norm`.
+    """A kfac_grad_item table (host memory; built once, reused every step), its scratch and the device float `norm`.  It stands for the memory
+    of these very tensors, which it keeps alive: gradients that are allocated anew need a new table.
     g: gradient tensors of any of the three types, their elements side by side; out: None (clipped in place), or per tensor None / a
     tensor of the same type, shape and strides that receives the clipped gradient.  A tensor that is written must not be there twice.
     Calls that use one table must not overlap in time."""

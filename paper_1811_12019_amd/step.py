@@ -243,7 +243,10 @@ class KfacExpertStep:
         P = layer.step()                                 factors, running averages, inverses, preconditioned gradients of layer.gradW
 
     gradW (experts, d_out, d_in) is the caller's to fill; step() clips P by the norm over all experts if max_norm is given (layer.norm is that
-    norm).  The running averages of an expert without tokens stay as they are."""
+    norm).  The running averages of an expert without tokens stay as they are.  An expert's factors are means over its own rows, A_e of the
+    tokens that came to it, G_e of the rows of dys, in which the weights are; its share of all tokens is in neither, so that the block of an
+    expert to which few come is damped as any other's.  The maps have no biases; for these, other scales or packed triangles call
+    kfac_expert_factor."""
 
     def __init__(self, tokens: int, choices: int, experts: int, d_in: int, d_out: int, dtype: torch.dtype = torch.bfloat16, decay: float = 0.95,
                  gamma: float = 1e-3, max_norm: Optional[float] = None, device="cuda"):
